@@ -440,6 +440,148 @@ int topoep_replica_grad_return(topoep_handle_t h, const int32_t* dev_replica_map
 int topoep_set_rank_window(topoep_handle_t h, int first_rank, int rank_count);
 
 /*
+ * ---------------------------------------------------------------------------------------------
+ * Operators of the MoE layer around a plan: the router that makes the ids a plan starts from, the
+ * expert layer of a few tokens on the instances a plan names, and the norm and clipping of the
+ * gradients that the replicas returned.  They stand outside the planner handle: the router takes
+ * its configuration by value in every call, the other two have handles of their own.  Like the
+ * planning calls they allocate no device memory, copy nothing to the host, never synchronise and
+ * only enqueue kernels (set_workspace excepted, as said there).
+ */
+enum { TOPOEP_DTYPE_F32 = 0, TOPOEP_DTYPE_BF16 = 1, TOPOEP_DTYPE_F16 = 2 };
+enum { TOPOEP_SCORE_SOFTMAX = 0, TOPOEP_SCORE_SIGMOID = 1 };
+
+typedef struct {
+  int32_t experts;     /* E in [1, 16384]                                                      */
+  int32_t top_k;       /* k in [1, min(E, 32)]                                                 */
+  int32_t dtype;       /* of the logits and of their gradient: TOPOEP_DTYPE_*                  */
+  int32_t score;       /* TOPOEP_SCORE_*                                                       */
+  int32_t normalize;   /* 1: the weights of a token's chosen experts sum to scale; else 0      */
+  float   scale;       /* factor on the weights: finite, > 0                                   */
+} topoep_router_config;
+
+/*
+ * Router, forward: for each token t the k experts with the largest choice value, in descending
+ * order, ties to the lowest expert id, and their weights.
+ *   choice_i = l_i (the logit), or sigma(l_i) + b_i when dev_bias is given (sigmoid scores only)
+ *   softmax:  w_j = scale * exp(l_j) / sum of exp(l_i) over the chosen (normalize) or all experts
+ *   sigmoid:  w_j = scale * sigma(l_j) [/ (sum of sigma over the chosen + 1e-20) (normalize)]
+ * An expert whose logit or choice value is -inf or NaN is never chosen.  A token with fewer than
+ * k experts left gets id -1 (what topoep_plan ignores) and weight 0 in the places left over; so
+ * does every place of a token whose dev_token_mask byte is 0.  Any other value, the type's lowest
+ * included, is an ordinary logit.  +inf and NaN follow IEEE arithmetic into the weights.
+ *   dev_logits     in  [tokens][E] of cfg->dtype, rows row_stride elements apart (>= E)
+ *   dev_bias       in  [E] float or NULL
+ *   dev_token_mask in  [tokens] bytes, 0 = leave the token out, or NULL
+ *   dev_topk_ids   out [tokens][k] int32, laid out as topoep_plan reads them
+ *   dev_weights    out [tokens][k] float
+ * Sums are held in 32 bits.  Enqueues one kernel.
+ */
+int topoep_router_forward(const topoep_router_config* cfg, const void* dev_logits,
+                          int64_t row_stride, int64_t tokens, const float* dev_bias,
+                          const uint8_t* dev_token_mask, int32_t* dev_topk_ids,
+                          float* dev_weights, topoep_stream_t stream);
+
+/*
+ * Router, backward: the gradient of the logits from that of the weights, with the ids and weights
+ * the forward call wrote.  With m = (1 / scale) * sum_j w_j dw_j over the chosen:
+ *   softmax, normalize:      dl_j = w_j (dw_j - m) at the chosen, 0 elsewhere
+ *   softmax over all:        dl_i = [i chosen] w_i dw_i - p_i scale m
+ *   sigmoid, normalize:      dl_j = w_j (1 - sigma(l_j)) (dw_j - m) at the chosen, 0 elsewhere
+ *   sigmoid:                 dl_j = w_j (1 - sigma(l_j)) dw_j at the chosen, 0 elsewhere
+ * Places with id -1 take no part; a token with no chosen expert has gradient 0.  An id outside
+ * [0, E) counts as -1.  The choice is piecewise constant and has no gradient, so a bias has none.
+ * dev_grad_logits [tokens][E] of cfg->dtype, rows grad_row_stride elements apart, is written in
+ * full.  It must not overlap the inputs.  Enqueues one kernel.
+ */
+int topoep_router_backward(const topoep_router_config* cfg, const void* dev_logits,
+                           int64_t row_stride, int64_t tokens, const int32_t* dev_topk_ids,
+                           const float* dev_weights, const float* dev_grad_weights,
+                           void* dev_grad_logits, int64_t grad_row_stride,
+                           topoep_stream_t stream);
+
+/*
+ * Expert layer of a few tokens (decoding, or the rows an EP rank received for one step):
+ *   y_t = sum_j w_tj * Wd[p](silu(Wg[p] x_t) * (Wu[p] x_t)),  p = dev_ids[t][j],
+ *   silu(a) = a / (1 + exp(-a)).
+ * p is a physical instance id as topoep_plan numbers them: with S_phys = experts_per_rank +
+ * slots_per_rank, p = r * S_phys + l is main block l of rank r for l < experts_per_rank, else
+ * replica slot l - experts_per_rank of rank r.  (With ranks = 1 and no slots p is just the expert
+ * id.)  The blocks are those of topoep_replica_pull: dev_main_params [ranks][experts_per_rank][W]
+ * and dev_replica_buf [ranks][slots_per_rank][W], W = 6 * hidden * ffn bytes, each block the
+ * bfloat16 matrices gate [ffn][hidden], up [ffn][hidden], down [hidden][ffn] in a row.
+ *
+ * topoep_experts_create: ranks >= 1, experts_per_rank >= 0, slots_per_rank >= 0, at least one and
+ * at most 8192 instances in all; hidden and ffn in [1, 65536]; top_k in [1, 16]; max_tokens in
+ * [1, 128].  Host memory only.
+ * topoep_experts_set_workspace: as topoep_set_workspace (256-byte aligned, stays the handle's,
+ * synchronises the device, outside stream capture).
+ * topoep_experts_set_params: where the blocks are; 16-byte aligned; either pointer may be NULL
+ * when it holds no block.  Host work only; may be called again when they move.
+ * topoep_experts_forward:
+ *   dev_x        in  [tokens][hidden] bfloat16, rows x_row_stride elements apart (>= hidden)
+ *   dev_ids      in  [tokens][k] int32; -1 is ignored in silence, any other value outside
+ *                    [0, instances) is ignored and sets TOPOEP_FLAG_BAD_ID
+ *   dev_weights  in  [tokens][k] float; the weight of an ignored id is not looked at
+ *   dev_y        out [tokens][hidden] bfloat16, rows y_row_stride elements apart (>= hidden); a
+ *                    token with no valid id gets zeros.  Must not overlap the inputs.
+ * The inner products are summed in 32 bits, the gated product between the two matrix products is
+ * held to 16 significant bits or more, the result is rounded once.  The order of the sums depends
+ * on sizes and ids only: the same call gives the same bits.  A block that no id names is not read, and a
+ * row's result depends on no other row's values.  Two calls on one handle must not overlap on the
+ * device.  Status bits are collected on the handle and read by topoep_experts_read_status
+ * (synchronises; clears them).
+ */
+typedef struct topoep_experts_ctx* topoep_experts_t;
+int topoep_experts_create(topoep_experts_t* out, int ranks, int experts_per_rank,
+                          int slots_per_rank, int hidden, int ffn, int top_k, int max_tokens);
+void topoep_experts_destroy(topoep_experts_t h);
+size_t topoep_experts_workspace_bytes(topoep_experts_t h);
+int topoep_experts_set_workspace(topoep_experts_t h, void* dev_ptr, size_t bytes);
+int topoep_experts_set_params(topoep_experts_t h, const void* dev_main_params,
+                              const void* dev_replica_buf);
+int topoep_experts_forward(topoep_experts_t h, const void* dev_x, int64_t x_row_stride,
+                           const int32_t* dev_ids, const float* dev_weights, int tokens,
+                           void* dev_y, int64_t y_row_stride, topoep_stream_t stream);
+int topoep_experts_read_status(topoep_experts_t h, uint32_t* host_flags);
+
+/*
+ * Global norm of many gradient tensors, and clipping (the step between the return of the replica
+ * gradients and the optimizer).
+ *   norm = sqrt(sum over all tensors of g^2)  (kind 0)   or   max |g|  (kind 1)
+ *   out  = g * min(1, max_norm / (norm + 1e-6)), rounded once to the tensor's type
+ * A NaN anywhere makes the norm NaN and every output NaN; an infinity makes the norm infinite and
+ * the factor 0 (the outputs 0, and NaN where g is infinite).  Squares are summed so that neither
+ * very large nor very small gradients leave the range of 32 bits (partial sums in 64 bits); the
+ * order of the sums depends on the sizes only.
+ *
+ * A tensor is rows of cols elements, src_row_stride / dst_row_stride elements apart (>= cols when
+ * rows > 1).  dst NULL or equal to src: in place (the strides have to agree).  Otherwise a dst
+ * overlaps no tensor.  Tensors with rows or cols 0 are left out.  Pointers need only their
+ * element's alignment.
+ *   topoep_clip_create        copies the list; count >= 0; host memory only
+ *   topoep_clip_set_workspace as topoep_set_workspace: uploads the list, synchronises the device
+ *   topoep_clip_norm          writes *dev_norm (float) only
+ *   topoep_clip_run           writes *dev_norm and every dst; max_norm >= 0
+ * Two calls on one handle must not overlap on the device.
+ */
+typedef struct topoep_clip_ctx* topoep_clip_t;
+typedef struct {
+  const void* src;
+  void* dst;
+  int64_t rows, cols, src_row_stride, dst_row_stride;
+  int32_t dtype;       /* TOPOEP_DTYPE_* */
+  int32_t reserved;
+} topoep_grad_tensor;
+int topoep_clip_create(topoep_clip_t* out, int64_t count, const topoep_grad_tensor* tensors);
+void topoep_clip_destroy(topoep_clip_t h);
+size_t topoep_clip_workspace_bytes(topoep_clip_t h);
+int topoep_clip_set_workspace(topoep_clip_t h, void* dev_ptr, size_t bytes);
+int topoep_clip_norm(topoep_clip_t h, int kind, float* dev_norm, topoep_stream_t stream);
+int topoep_clip_run(topoep_clip_t h, int kind, float max_norm, float* dev_norm,
+                    topoep_stream_t stream);
+
+/*
  * Number of kernels topoep_plan would enqueue for a call of this size with the
  * current knobs: 5, 4 or 2 (see TOPOEP_KNOB_CHAIN).  Needs the
  * workspace (the answer depends on the device).  Negative status on a bad

@@ -25,7 +25,15 @@ EXPORTS = ("topoep_create", "topoep_destroy", "topoep_workspace_bytes", "topoep_
            "topoep_summary", "topoep_read_status",
            "topoep_debug_tensor", "topoep_set_tuning", "topoep_set_rank_window", "topoep_set_policy", "topoep_replica_pull", "topoep_replica_grad_return",
            "topoep_get_layout", "topoep_plan_kernels", "topoep_plan_byte_copy",
-           "topoep_launch_floor", "topoep_strerror")
+           "topoep_launch_floor", "topoep_strerror",
+           "topoep_router_forward", "topoep_router_backward",
+           "topoep_experts_create", "topoep_experts_destroy", "topoep_experts_workspace_bytes",
+           "topoep_experts_set_workspace", "topoep_experts_set_params", "topoep_experts_forward",
+           "topoep_experts_read_status",
+           "topoep_clip_create", "topoep_clip_destroy", "topoep_clip_workspace_bytes",
+           "topoep_clip_set_workspace", "topoep_clip_norm", "topoep_clip_run")
+DTYPE_F32, DTYPE_BF16, DTYPE_F16 = 0, 1, 2
+SCORE_SOFTMAX, SCORE_SIGMOID = 0, 1
 
 
 class CostParams(ctypes.Structure):
@@ -41,6 +49,18 @@ class Summary(ctypes.Structure):
                  "replicas_intra", "t_comp", "t_token", "t_replica", "cross_token_bytes",
                  "refine_iters", "reserved")] + \
                [(n, ctypes.c_double) for n in ("imbalance", "cross_fraction", "replica_fraction")]
+
+
+class RouterConfig(ctypes.Structure):
+    _fields_ = [("experts", ctypes.c_int32), ("top_k", ctypes.c_int32), ("dtype", ctypes.c_int32),
+                ("score", ctypes.c_int32), ("normalize", ctypes.c_int32), ("scale", ctypes.c_float)]
+
+
+class GradTensor(ctypes.Structure):
+    _fields_ = [("src", ctypes.c_void_p), ("dst", ctypes.c_void_p), ("rows", ctypes.c_int64),
+                ("cols", ctypes.c_int64), ("src_row_stride", ctypes.c_int64),
+                ("dst_row_stride", ctypes.c_int64), ("dtype", ctypes.c_int32),
+                ("reserved", ctypes.c_int32)]
 
 
 _lib = None
@@ -112,6 +132,33 @@ def lib() -> ctypes.CDLL:
         L.topoep_plan_byte_copy.argtypes = [vp, ci, ci]
         L.topoep_launch_floor.restype = ci
         L.topoep_launch_floor.argtypes = [ci, vp]
+        sz, i64 = ctypes.c_size_t, ctypes.c_int64
+        cfgp = ctypes.POINTER(RouterConfig)
+        L.topoep_router_forward.restype = ci
+        L.topoep_router_forward.argtypes = [cfgp, vp, i64, i64, vp, vp, vp, vp, vp]
+        L.topoep_router_backward.restype = ci
+        L.topoep_router_backward.argtypes = [cfgp, vp, i64, i64, vp, vp, vp, vp, i64, vp]
+        L.topoep_experts_create.restype = ci
+        L.topoep_experts_create.argtypes = [ctypes.POINTER(vp)] + [ci] * 7
+        L.topoep_experts_forward.restype = ci
+        L.topoep_experts_forward.argtypes = [vp, vp, i64, vp, vp, ci, vp, i64, vp]
+        L.topoep_experts_set_params.restype = ci
+        L.topoep_experts_set_params.argtypes = [vp, vp, vp]
+        L.topoep_experts_read_status.restype = ci
+        L.topoep_experts_read_status.argtypes = [vp, ctypes.POINTER(ctypes.c_uint32)]
+        L.topoep_clip_create.restype = ci
+        L.topoep_clip_create.argtypes = [ctypes.POINTER(vp), i64, ctypes.POINTER(GradTensor)]
+        L.topoep_clip_norm.restype = ci
+        L.topoep_clip_norm.argtypes = [vp, ci, vp, vp]
+        L.topoep_clip_run.restype = ci
+        L.topoep_clip_run.argtypes = [vp, ci, ctypes.c_float, vp, vp]
+        for name in ("experts", "clip"):
+            fn = getattr(L, "topoep_%s_destroy" % name)
+            fn.restype, fn.argtypes = None, [vp]
+            fn = getattr(L, "topoep_%s_workspace_bytes" % name)
+            fn.restype, fn.argtypes = sz, [vp]
+            fn = getattr(L, "topoep_%s_set_workspace" % name)
+            fn.restype, fn.argtypes = ci, [vp, vp, sz]
         L.topoep_strerror.restype = ctypes.c_char_p
         L.topoep_strerror.argtypes = [ci]
         _lib = L
@@ -282,3 +329,86 @@ def topoep_plan_byte_copy(h, tokens_per_rank: int, batch: int) -> int:
 
 def topoep_launch_floor(count: int, stream=0) -> int:
     return lib().topoep_launch_floor(count, stream or None)
+
+
+def topoep_router_forward(cfg: RouterConfig, dev_logits, row_stride, tokens, dev_bias,
+                          dev_token_mask, dev_topk_ids, dev_weights, stream=0) -> int:
+    return lib().topoep_router_forward(ctypes.byref(cfg) if cfg is not None else None,
+                                       _ptr(dev_logits), row_stride, tokens, _ptr(dev_bias),
+                                       _ptr(dev_token_mask), _ptr(dev_topk_ids),
+                                       _ptr(dev_weights), stream or None)
+
+
+def topoep_router_backward(cfg: RouterConfig, dev_logits, row_stride, tokens, dev_topk_ids,
+                           dev_weights, dev_grad_weights, dev_grad_logits, grad_row_stride,
+                           stream=0) -> int:
+    return lib().topoep_router_backward(ctypes.byref(cfg) if cfg is not None else None,
+                                        _ptr(dev_logits), row_stride, tokens, _ptr(dev_topk_ids),
+                                        _ptr(dev_weights), _ptr(dev_grad_weights),
+                                        _ptr(dev_grad_logits), grad_row_stride, stream or None)
+
+
+def topoep_experts_create(ranks, experts_per_rank, slots_per_rank, hidden, ffn, top_k, max_tokens):
+    """Returns (status, handle)."""
+    h = ctypes.c_void_p()
+    rc = lib().topoep_experts_create(ctypes.byref(h), ranks, experts_per_rank, slots_per_rank,
+                                     hidden, ffn, top_k, max_tokens)
+    return rc, (h if rc == OK else None)
+
+
+def topoep_experts_destroy(h) -> None:
+    lib().topoep_experts_destroy(h)
+
+
+def topoep_experts_workspace_bytes(h) -> int:
+    return int(lib().topoep_experts_workspace_bytes(h))
+
+
+def topoep_experts_set_workspace(h, dev_ptr, nbytes: int) -> int:
+    return lib().topoep_experts_set_workspace(h, _ptr(dev_ptr), nbytes)
+
+
+def topoep_experts_set_params(h, dev_main_params, dev_replica_buf) -> int:
+    return lib().topoep_experts_set_params(h, _ptr(dev_main_params), _ptr(dev_replica_buf))
+
+
+def topoep_experts_forward(h, dev_x, x_row_stride, dev_ids, dev_weights, tokens, dev_y,
+                           y_row_stride, stream=0) -> int:
+    return lib().topoep_experts_forward(h, _ptr(dev_x), x_row_stride, _ptr(dev_ids),
+                                        _ptr(dev_weights), tokens, _ptr(dev_y), y_row_stride,
+                                        stream or None)
+
+
+def topoep_experts_read_status(h):
+    """Returns (status, flags)."""
+    f = ctypes.c_uint32(0)
+    rc = lib().topoep_experts_read_status(h, ctypes.byref(f))
+    return rc, int(f.value)
+
+
+def topoep_clip_create(tensors):
+    """tensors: a sequence of GradTensor.  Returns (status, handle)."""
+    h = ctypes.c_void_p()
+    arr = (GradTensor * max(len(tensors), 1))(*tensors)
+    rc = lib().topoep_clip_create(ctypes.byref(h), len(tensors), arr)
+    return rc, (h if rc == OK else None)
+
+
+def topoep_clip_destroy(h) -> None:
+    lib().topoep_clip_destroy(h)
+
+
+def topoep_clip_workspace_bytes(h) -> int:
+    return int(lib().topoep_clip_workspace_bytes(h))
+
+
+def topoep_clip_set_workspace(h, dev_ptr, nbytes: int) -> int:
+    return lib().topoep_clip_set_workspace(h, _ptr(dev_ptr), nbytes)
+
+
+def topoep_clip_norm(h, kind: int, dev_norm, stream=0) -> int:
+    return lib().topoep_clip_norm(h, kind, _ptr(dev_norm), stream or None)
+
+
+def topoep_clip_run(h, kind: int, max_norm: float, dev_norm, stream=0) -> int:
+    return lib().topoep_clip_run(h, kind, max_norm, _ptr(dev_norm), stream or None)

@@ -1,0 +1,351 @@
+"""Operators of an MoE layer around a plan: router, experts of a few tokens, gradient clipping.
+
+Marshalling only, like `planner`: arguments are checked, outputs and workspaces are torch tensors,
+and every step runs in the CUDA library on the caller's stream.
+"""
+from __future__ import annotations
+
+from typing import Optional, Sequence
+
+import torch
+
+from . import binding as B
+
+_DTYPES = {torch.float32: B.DTYPE_F32, torch.bfloat16: B.DTYPE_BF16, torch.float16: B.DTYPE_F16}
+
+
+def _check(ok: bool, what: str):
+    if not ok:
+        raise ValueError(what)
+
+
+def _raise(rc: int):
+    if rc != B.OK:
+        raise B.TopoEPError(rc)
+
+
+class _On:
+    """The stream and device a call runs on: the caller's stream, or the current one of the
+    device.  Tensors the call allocates belong to that stream, and tensors it is given are marked
+    as used there, so that their memory is not handed out again before the call is done."""
+
+    def __init__(self, device: torch.device, stream: Optional[torch.cuda.Stream], given=()):
+        self.device = device
+        self.index = device.index
+        current = torch.cuda.current_stream(device)
+        self.raw = current.cuda_stream if stream is None else stream.cuda_stream
+        self.guard = None
+        if stream is not None and stream.cuda_stream != current.cuda_stream:
+            _check(stream.device_index == self.index, "the stream belongs to another device")
+            self.guard = torch.cuda.stream(stream)
+            for t in given:
+                if t is not None:
+                    t.record_stream(stream)
+        elif torch.cuda.current_device() != self.index:
+            self.guard = torch.cuda.device(self.index)
+
+    def __enter__(self):
+        if self.guard is not None:
+            self.guard.__enter__()
+        return self.raw
+
+    def __exit__(self, *exc):
+        if self.guard is not None:
+            self.guard.__exit__(*exc)
+
+
+def _workspace(nbytes: int, device: torch.device):
+    """(tensor, 256-byte aligned address) of a workspace."""
+    t = torch.empty(nbytes + 256, dtype=torch.uint8, device=device)
+    return t, (t.data_ptr() + 255) // 256 * 256
+
+
+class _RouterFunction(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, logits, bias, mask, router):
+        ids, weights = router.forward(logits, bias=bias, mask=mask)
+        ctx.save_for_backward(logits, ids, weights)
+        ctx.router = router
+        ctx.mark_non_differentiable(ids)
+        return ids, weights
+
+    @staticmethod
+    def backward(ctx, _, grad_weights):
+        logits, ids, weights = ctx.saved_tensors
+        return ctx.router.backward(logits, ids, weights, grad_weights), None, None, None
+
+
+class Router:
+    """topoep_router_forward / topoep_router_backward for one layer's configuration.
+
+    score: "softmax" or "sigmoid"; normalize: the weights of a token's chosen experts sum to
+    `scale`.  Calling the object differentiates through torch.autograd; forward() and backward()
+    are the two directions alone."""
+
+    def __init__(self, experts: int, top_k: int, score: str = "softmax", normalize: bool = True,
+                 scale: float = 1.0):
+        _check(score in ("softmax", "sigmoid"), "score is 'softmax' or 'sigmoid'")
+        self.experts, self.top_k, self.score = int(experts), int(top_k), score
+        self.normalize, self.scale = bool(normalize), float(scale)
+        self._cfg = {d: B.RouterConfig(self.experts, self.top_k, code,
+                                       B.SCORE_SIGMOID if score == "sigmoid" else B.SCORE_SOFTMAX,
+                                       int(self.normalize), self.scale)
+                     for d, code in _DTYPES.items()}
+        # the configuration's own errors, without a device
+        _raise(B.topoep_router_forward(self._cfg[torch.float32], None, self.experts, 0, None, None,
+                                       None, None))
+
+    def _rows(self, t: torch.Tensor, what: str) -> torch.Tensor:
+        _check(t.is_cuda and t.dtype in _DTYPES, what + ": a float32, bfloat16 or float16 CUDA tensor")
+        _check(t.dim() >= 1 and t.shape[-1] == self.experts,
+               "%s: the last dimension has %d experts" % (what, self.experts))
+        if t.dim() != 2:
+            t = t.reshape(-1, self.experts)
+        _check(t.shape[1] <= 1 or t.stride(1) == 1, what + ": experts of a token are adjacent")
+        _check(t.shape[0] <= 1 or t.stride(0) >= self.experts, what + ": rows do not overlap")
+        return t
+
+    def _stride(self, t: torch.Tensor) -> int:
+        return t.stride(0) if t.shape[0] > 1 else self.experts
+
+    def forward(self, logits: torch.Tensor, bias: Optional[torch.Tensor] = None,
+                mask: Optional[torch.Tensor] = None, stream=None):
+        """(ids int32, weights float32), each [...][top_k], of logits [...][experts].
+
+        bias [experts] float32 is added to the sigmoid scores for the choice alone; mask [...]
+        (bool or uint8) leaves out the tokens where it is 0: ids -1, weights 0."""
+        rows = self._rows(logits, "logits")
+        T, lead = rows.shape[0], logits.shape[:-1]
+        if bias is not None:
+            _check(bias.dtype == torch.float32 and bias.is_contiguous() and
+                   bias.device == rows.device and tuple(bias.shape) == (self.experts,),
+                   "bias: [experts] float32, contiguous, on the logits' device")
+        if mask is not None:
+            _check(mask.dtype in (torch.bool, torch.uint8) and mask.is_contiguous() and
+                   mask.device == rows.device and mask.shape == lead,
+                   "mask: bool or uint8, contiguous, one value a token, on the logits' device")
+        with _On(rows.device, stream, (logits, bias, mask)) as raw:
+            ids = torch.empty(lead + (self.top_k,), dtype=torch.int32, device=rows.device)
+            weights = torch.empty(lead + (self.top_k,), dtype=torch.float32, device=rows.device)
+            _raise(B.topoep_router_forward(self._cfg[rows.dtype], rows, self._stride(rows), T, bias,
+                                           mask, ids, weights, raw))
+        return ids, weights
+
+    def backward(self, logits: torch.Tensor, ids: torch.Tensor, weights: torch.Tensor,
+                 grad_weights: torch.Tensor, stream=None) -> torch.Tensor:
+        """Gradient of the logits (their type and shape) from the gradient of the weights."""
+        rows = self._rows(logits, "logits")
+        T, want = rows.shape[0], logits.shape[:-1] + (self.top_k,)
+        _check(ids.dtype == torch.int32 and ids.is_contiguous() and ids.shape == want and
+               ids.device == rows.device, "ids: as forward() returned them")
+        _check(weights.dtype == torch.float32 and weights.is_contiguous() and
+               weights.shape == want and weights.device == rows.device,
+               "weights: as forward() returned them")
+        _check(grad_weights.dtype == torch.float32 and grad_weights.shape == want and
+               grad_weights.device == rows.device, "grad_weights: float32, shaped as the weights")
+        with _On(rows.device, stream, (logits, ids, weights, grad_weights)) as raw:
+            grad_weights = grad_weights.contiguous()
+            grad = torch.empty(logits.shape, dtype=rows.dtype, device=rows.device)
+            _raise(B.topoep_router_backward(self._cfg[rows.dtype], rows, self._stride(rows), T, ids,
+                                            weights, grad_weights, grad, self.experts, raw))
+        return grad
+
+    def __call__(self, logits: torch.Tensor, bias: Optional[torch.Tensor] = None,
+                 mask: Optional[torch.Tensor] = None):
+        return _RouterFunction.apply(logits, bias, mask, self)
+
+
+class TokenExperts:
+    """topoep_experts_* : the expert layer of at most `max_tokens` tokens on the current CUDA
+    device, on the parameter blocks of Planner.replica_pull."""
+
+    def __init__(self, hidden: int, ffn: int, top_k: int, max_tokens: int, experts_per_rank: int,
+                 slots_per_rank: int = 0, ranks: int = 1, device: Optional[torch.device] = None):
+        self.handle = None
+        self.hidden, self.ffn, self.top_k, self.max_tokens = hidden, ffn, top_k, max_tokens
+        self.ranks, self.e_loc, self.slots = ranks, experts_per_rank, slots_per_rank
+        self.block_bytes = 6 * hidden * ffn
+        rc, handle = B.topoep_experts_create(ranks, experts_per_rank, slots_per_rank, hidden, ffn,
+                                             top_k, max_tokens)
+        _raise(rc)
+        self.handle = handle
+        if not torch.cuda.is_available():
+            raise RuntimeError("the expert layer needs a CUDA device; there is no CPU path")
+        self.device = torch.device(device) if device is not None else torch.device("cuda")
+        if self.device.index is None:
+            self.device = torch.device("cuda", torch.cuda.current_device())
+        self._params = None
+        nbytes = B.topoep_experts_workspace_bytes(handle)
+        with torch.cuda.device(self.device):
+            self._workspace, ptr = _workspace(nbytes, self.device)
+            _raise(B.topoep_experts_set_workspace(handle, ptr, nbytes))
+
+    def close(self):
+        if getattr(self, "handle", None) is not None:
+            B.topoep_experts_destroy(self.handle)
+            self.handle = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:   # interpreter shutdown: the binding module may already be gone
+            pass
+
+    def set_experts(self, main_params: Optional[torch.Tensor],
+                    replica_buf: Optional[torch.Tensor] = None):
+        """The blocks: main_params [ranks][experts_per_rank][W] and replica_buf
+        [ranks][slots_per_rank][W], uint8 with W = 6 * hidden * ffn bytes (or bfloat16, W / 2
+        elements), contiguous; they are used where they lie."""
+        for t, n, what in ((main_params, self.e_loc, "main_params"),
+                           (replica_buf, self.slots, "replica_buf")):
+            if n == 0:
+                continue
+            _check(t is not None, what + " is needed")
+            _check(t.dtype in (torch.uint8, torch.bfloat16) and t.is_contiguous() and
+                   t.device == self.device and
+                   t.numel() * t.element_size() == self.ranks * n * self.block_bytes,
+                   "%s: uint8 or bfloat16, contiguous, on this device, %d blocks of %d bytes"
+                   % (what, self.ranks * n, self.block_bytes))
+        main = main_params if self.e_loc else None
+        replica = replica_buf if self.slots else None
+        with torch.cuda.device(self.device):
+            _raise(B.topoep_experts_set_params(self.handle, main, replica))
+        self._params = (main, replica)
+
+    def forward(self, x: torch.Tensor, ids: torch.Tensor, weights: torch.Tensor,
+                out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+        """y [tokens][hidden] bfloat16 of x [tokens][hidden] bfloat16, instance ids [tokens][top_k]
+        int32 (the plan's token_replica rows) and weights [tokens][top_k] float32."""
+        _check(x.dim() == 2 and x.dtype == torch.bfloat16 and x.shape[1] == self.hidden and
+               x.device == self.device, "x: [tokens][hidden] bfloat16 on this device")
+        T = x.shape[0]
+        _check(T <= self.max_tokens, "at most %d tokens" % self.max_tokens)
+        _check(x.shape[1] == 1 or x.stride(1) == 1, "x: elements of a row are adjacent")
+        _check(T <= 1 or x.stride(0) >= self.hidden or x.stride(0) == 0, "x: rows do not overlap")
+        if T > 1 and x.stride(0) == 0:   # one row for every token
+            x = x.contiguous()
+        want = (T, self.top_k)
+        _check(ids.dtype == torch.int32 and ids.is_contiguous() and tuple(ids.shape) == want and
+               ids.device == self.device, "ids: [tokens][top_k] int32, contiguous, on this device")
+        _check(weights.dtype == torch.float32 and weights.is_contiguous() and
+               tuple(weights.shape) == want and weights.device == self.device,
+               "weights: [tokens][top_k] float32, contiguous, on this device")
+        with _On(self.device, stream, (x, ids, weights, out)) as raw:
+            if out is None:
+                out = torch.empty((T, self.hidden), dtype=torch.bfloat16, device=self.device)
+            else:
+                _check(out.dtype == torch.bfloat16 and tuple(out.shape) == (T, self.hidden) and
+                       out.device == self.device and (self.hidden == 1 or out.stride(1) == 1) and
+                       (T <= 1 or out.stride(0) >= self.hidden),
+                       "out: [tokens][hidden] bfloat16 on this device, elements of a row adjacent")
+            _raise(B.topoep_experts_forward(self.handle, x, x.stride(0) if T > 1 else self.hidden,
+                                            ids, weights, T, out,
+                                            out.stride(0) if T > 1 else self.hidden, raw))
+        return out
+
+    __call__ = forward
+
+    def status(self) -> int:
+        with torch.cuda.device(self.device):
+            rc, flags = B.topoep_experts_read_status(self.handle)
+        _raise(rc)
+        return flags
+
+
+def _rows_of(t: torch.Tensor):
+    """(dimension order, rows, cols, row stride) of a tensor whose elements lie in rows of adjacent
+    ones, in whatever order of its dimensions; None if they do not."""
+    order = sorted((d for d in range(t.dim()) if t.shape[d] != 1), key=t.stride)
+    cols, at = 1, 0
+    while at < len(order) and t.stride(order[at]) == cols:
+        cols *= t.shape[order[at]]
+        at += 1
+    rows, stride = 1, cols
+    for d in order[at:]:
+        if rows == 1:
+            rows, stride = t.shape[d], t.stride(d)
+        elif t.stride(d) == rows * stride:
+            rows *= t.shape[d]
+        else:
+            return None
+    return (order, rows, cols, stride) if stride >= cols else None
+
+
+def _pair(g: torch.Tensor, o: torch.Tensor):
+    """(rows, cols, row stride of g, row stride of o), or None when the two do not lie alike."""
+    a, b = _rows_of(g), _rows_of(o)
+    if a is None or b is None or a[0] != b[0]:
+        return None
+    if a[1] == 1 and b[1] > 1:     # one run: cut like the other
+        a = (a[0], b[1], b[2], b[2])
+    elif b[1] == 1 and a[1] > 1:
+        b = (b[0], a[1], a[2], a[2])
+    return (a[1], a[2], a[3], b[3]) if a[1:3] == b[1:3] else None
+
+
+class GradientClip:
+    """topoep_clip_* : global norm and clipping of a fixed list of gradient tensors.
+
+    The list is laid out once; the tensors may change their values, not their place.  out: tensors
+    of the same shapes, types and strides for the clipped gradients (default: in place).  norm:
+    "l2" or "max"."""
+
+    def __init__(self, grads: Sequence[torch.Tensor], out: Optional[Sequence[torch.Tensor]] = None,
+                 norm: str = "l2"):
+        self.handle = None
+        grads = list(grads)
+        outs = grads if out is None else list(out)
+        _check(norm in ("l2", "max"), "norm is 'l2' or 'max'")
+        _check(len(outs) == len(grads), "as many outputs as gradients")
+        _check(len(grads) > 0, "at least one gradient")
+        self._kind = 0 if norm == "l2" else 1
+        self.device = grads[0].device
+        table = []
+        for g, o in zip(grads, outs):
+            _check(g.is_cuda and g.device == self.device and g.dtype in _DTYPES,
+                   "gradients: float32, bfloat16 or float16 CUDA tensors of one device")
+            _check(o.device == self.device and o.dtype == g.dtype and o.shape == g.shape,
+                   "an output has its gradient's device, type and shape")
+            if g.numel() == 0:
+                continue
+            lie = _pair(g, o)
+            _check(lie is not None, "a gradient's elements lie in rows of adjacent elements, one "
+                   "distance between the rows, and its output's in the same order")
+            table.append(B.GradTensor(g.data_ptr(), o.data_ptr(), *lie, _DTYPES[g.dtype], 0))
+        self._tensors = (grads, outs)
+        rc, handle = B.topoep_clip_create(table)
+        _raise(rc)
+        self.handle = handle
+        nbytes = B.topoep_clip_workspace_bytes(handle)
+        with torch.cuda.device(self.device):
+            self._workspace, ptr = _workspace(nbytes, self.device)
+            _raise(B.topoep_clip_set_workspace(handle, ptr, nbytes))
+
+    def close(self):
+        if getattr(self, "handle", None) is not None:
+            B.topoep_clip_destroy(self.handle)
+            self.handle = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:   # interpreter shutdown: the binding module may already be gone
+            pass
+
+    def norm(self, stream=None) -> torch.Tensor:
+        """The global norm, a float32 scalar on the device."""
+        return self._call(None, stream)
+
+    def clip(self, max_norm: float, stream=None) -> torch.Tensor:
+        """Scales the gradients to at most max_norm; returns the norm before clipping."""
+        return self._call(float(max_norm), stream)
+
+    def _call(self, max_norm, stream):
+        given = () if stream is None else [t for both in self._tensors for t in both]
+        with _On(self.device, stream, given) as raw:
+            value = torch.empty((), dtype=torch.float32, device=self.device)
+            if max_norm is None:
+                _raise(B.topoep_clip_norm(self.handle, self._kind, value, raw))
+            else:
+                _raise(B.topoep_clip_run(self.handle, self._kind, max_norm, value, raw))
+        return value

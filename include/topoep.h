@@ -530,7 +530,8 @@ int topoep_router_backward(const topoep_router_config* cfg, const void* dev_logi
  * on sizes and ids only: the same call gives the same bits.  A block that no id names is not read, and a
  * row's result depends on no other row's values.  Two calls on one handle must not overlap on the
  * device.  Status bits are collected on the handle and read by topoep_experts_read_status
- * (synchronises; clears them).
+ * (synchronises; clears them).  TOPOEP_FLAG_INTERNAL means that a bounded wait ran out: the result
+ * is void and the workspace has to be set again.
  */
 typedef struct topoep_experts_ctx* topoep_experts_t;
 int topoep_experts_create(topoep_experts_t* out, int ranks, int experts_per_rank,

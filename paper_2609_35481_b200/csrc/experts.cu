@@ -1,7 +1,34 @@
 // Expert layer of a few tokens on the physical instances a plan names (definition in topoep.h).
 //
 // Bound by memory: every block that some id names is read once, 6 * hidden * ffn bytes, and meets
-// at most a few tokens.
+// at most a few tokens.  One persistent kernel, one CTA an SM, does the whole layer:
+//
+//   0. Every CTA groups the ids by instance: a bit mask of tokens for each instance, a scan over
+//      the instances, the named ones numbered in ascending order ("slots"), their tokens in
+//      ascending order ("rows" of the scratch).  Same ids, same numbering in every CTA.
+//   1. Gate and up.  The weights are the M side of the matrix product (128 gate rows and the 128 up
+//      rows of the same outputs), the tokens of the instance the N side (16 to 128 columns), so
+//      the tensor core's tile is full whatever the number of tokens and every weight passes
+//      through shared memory once.  The rows of x are gathered by the copy unit (four rows a
+//      copy).  h = silu(g) * u goes to the scratch as two bfloat16 numbers, the rounded value and
+//      the rounded rest: 16 significant bits.
+//   2. Down.  Same product with 256 rows of the down matrix and the two parts of h, both summed
+//      into the same accumulator; partial results per row go to the scratch in 32 bits.
+//   3. Every token's rows are weighted and summed, in the order of its ids.
+//
+// The work of 1 and of 2 is a list of (slot, tile of rows, step of 64 along the sum) units, cut into
+// one equal run of units for each CTA, so that all SMs stream the same number of bytes whatever
+// the sizes.  A tile cut between CTAs is summed from partial accumulators in the order of the CTAs:
+// in 1 by the CTA that finishes last (it needs the whole sum before the activation), in 2 by step 3.
+// Between 1 and 2 only the copies of h wait: the copies of the weights, issued by another warp, run
+// ahead and keep the memory busy while the last tiles of 1 are finished.
+//
+// Roles of a CTA's eight warps: 0 copies weights, 1 copies token rows, 2 issues the products, 4-7
+// read the accumulators (double-buffered in tensor memory).  The launch is cooperative: every CTA
+// is resident, so the waits of 2 and 3 end; all waits are bounded all the same and set
+// TOPOEP_FLAG_INTERNAL when they run out.
+#include <cuda.h>
+
 #include <algorithm>
 #include <new>
 
@@ -78,8 +105,606 @@ __global__ void __launch_bounds__(kAnyThreads) experts_down_any_kernel(const Exp
   if (lane == 0) p.y[t * p.y_stride + c] = __float2bfloat16_rn(y);
 }
 
+// ------------------------------------------------------------------- the tensor-core kernel
+
+constexpr int kThreads = 256;
+constexpr int kTileM = 128;             // rows of one product; a stage holds two
+constexpr int kStepK = 64;              // elements of the sum in a step: one 128-byte swizzled row
+constexpr int kHalfBytes = kTileM * kStepK * 2;
+constexpr int kStageA = 2 * kHalfBytes;
+constexpr int kMaxStages = 8;
+constexpr unsigned kWaitLimit = 1u << 25;   // polls of a wait (about a second) before it is given up
+constexpr unsigned kSpinLimit = 1u << 22;   // polls of a word in global memory (a few seconds)
+
+// Words of the workspace's control block (zero between calls).
+enum { C_STATUS = 0, C_TILES = 16, C_ARRIVE = 32, C_LEAVE = 48, C_WORDS = 64 };
+
+struct __align__(64) Maps {
+  CUtensorMap main_gu, main_down, replica_gu, replica_down, x, h;
+};
+
+struct LayerParams {
+  const int32_t* ids;
+  const float* weights;
+  __nv_bfloat16* y;
+  uint32_t* control;
+  unsigned* tile_steps;      // [slots * tiles of phase 1] steps of a cut tile already summed
+  float* partial;            // [CTA][2][column][256]
+  __nv_bfloat16* h;          // [2][rows][F]: rounded value, rounded rest
+  float* yp;                 // [plane][row][H]
+  long long y_stride;
+  int tokens, k, H, F, e_loc, slots, instances, max_rows;
+  int stages, stage_bytes, b_half;   // b_half: bytes of the columns' side (one part)
+  int tmem_cols, acc_cols;
+  int o_act, o_off, o_tok, o_pos, o_slot;   // offsets of the tables behind the ring
+};
+
+__device__ __forceinline__ uint32_t smem_u32(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
+
+__device__ __forceinline__ void mbar_init(uint32_t bar, uint32_t count) {
+  asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count) : "memory");
+}
+__device__ __forceinline__ void mbar_expect(uint32_t bar, uint32_t bytes) {
+  asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ void mbar_arrive(uint32_t bar) {
+  asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
+}
+__device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity) {
+  for (unsigned i = 0; i < kWaitLimit; ++i) {
+    uint32_t done;
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "mbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
+        "selp.u32 %0, 1, 0, p;\n\t}"
+        : "=r"(done) : "r"(bar), "r"(parity) : "memory");
+    if (done) return true;
+  }
+  return false;
+}
+__device__ __forceinline__ void tma_weights(uint32_t dst, const CUtensorMap* map, int x, int y, int z, uint32_t bar) {
+  asm volatile(
+      "cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];"
+      ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(z), "r"(bar) : "memory");
+}
+__device__ __forceinline__ void tma_rows(uint32_t dst, const CUtensorMap* map, int x, int r0, int r1, int r2, int r3,
+                                         uint32_t bar) {
+  asm volatile(
+      "cp.async.bulk.tensor.2d.shared::cluster.global.tile::gather4.mbarrier::complete_tx::bytes "
+      "[%0], [%1, {%2, %3, %4, %5, %6}], [%7];"
+      ::"r"(dst), "l"(map), "r"(x), "r"(r0), "r"(r1), "r"(r2), "r"(r3), "r"(bar) : "memory");
+}
+// Shared-memory operand: K-major rows of 128 bytes in the 128-byte swizzle, 8-row groups 1024 apart.
+__device__ __forceinline__ uint64_t operand(uint32_t addr) {
+  return (uint64_t)(addr >> 4) | (1ull << 16) | (64ull << 32) | (1ull << 46) | (2ull << 61);
+}
+__device__ __forceinline__ void mma(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t add) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
+      ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(add) : "memory");
+}
+__device__ __forceinline__ void mma_commit(uint32_t bar) {
+  asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
+}
+__device__ __forceinline__ void tmem_load16(uint32_t addr, float (&v)[16]) {
+  uint32_t r[16];
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
+        "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+      : "r"(addr));
+#pragma unroll
+  for (int i = 0; i < 16; ++i) v[i] = __uint_as_float(r[i]);
+}
+__device__ __forceinline__ unsigned load_acquire(const unsigned* p) {
+  unsigned v;
+  asm volatile("ld.acquire.gpu.global.u32 %0, [%1];" : "=r"(v) : "l"(p) : "memory");
+  return v;
+}
+__device__ __forceinline__ void add_release(unsigned* p, unsigned v) {
+  asm volatile("red.release.gpu.global.add.u32 [%0], %1;" ::"l"(p), "r"(v) : "memory");
+}
+__device__ __forceinline__ bool spin_until(const unsigned* p, unsigned want) {
+  for (unsigned i = 0; i < kSpinLimit; ++i)
+    if (load_acquire(p) == want) return true;
+  return false;
+}
+__device__ __forceinline__ void epilogue_sync() { asm volatile("bar.sync 1, 128;" ::: "memory"); }
+
+// The units of a phase and their division into one run a CTA.
+struct Runs {
+  int tiles, steps, per_slot, q, r;
+  __device__ Runs(int slots, int per_slot_, int steps_) {
+    per_slot = per_slot_;
+    steps = steps_;
+    tiles = slots * per_slot_;
+    const int units = tiles * steps;
+    q = units / (int)gridDim.x;
+    r = units - q * (int)gridDim.x;
+  }
+  __device__ int start(int c) const { return c * q + min(c, r); }
+  __device__ int cta_of(int u) const { return u < r * (q + 1) ? u / (q + 1) : r + (u - r * (q + 1)) / q; }
+};
+
+// One stretch of a tile that a CTA works on.
+struct Piece {
+  int tile, slot, m, k0, k1;
+};
+
+struct PieceWalk {
+  const Runs& runs;
+  int u, end;
+  __device__ PieceWalk(const Runs& r, int cta) : runs(r), u(r.start(cta)), end(r.start(cta + 1)) {}
+  __device__ bool next(Piece& p) {
+    if (u >= end) return false;
+    p.tile = u / runs.steps;
+    p.k0 = u - p.tile * runs.steps;
+    p.k1 = min(runs.steps, p.k0 + end - u);
+    p.slot = p.tile / runs.per_slot;
+    p.m = p.tile - p.slot * runs.per_slot;
+    u += p.k1 - p.k0;
+    return true;
+  }
+};
+
+struct Tables {
+  const uint16_t* act;   // [slots] instance
+  const uint16_t* off;   // [slots + 1] first row
+  const uint8_t* tok;    // [rows] token
+  const uint16_t* pos;   // [tokens * k] row of an assignment, 0xffff: ignored
+  const uint16_t* slot;  // [tokens * k] its slot
+};
+
+__device__ __forceinline__ void store_h(const LayerParams& p, int row, int f, float g, float u) {
+  const float h = g / (1.0f + expf(-g)) * u;
+  const __nv_bfloat16 hi = __float2bfloat16_rn(h);
+  // the rest of an infinity or NaN is 0: the first part says it all
+  const float rest = h - to_f32(hi);
+  p.h[(size_t)row * p.F + f] = hi;
+  p.h[((size_t)p.max_rows + row) * p.F + f] = __float2bfloat16_rn(isfinite(rest) ? rest : 0.0f);
+}
+
+__global__ void __launch_bounds__(kThreads, 1)
+experts_kernel(const __grid_constant__ Maps maps, const __grid_constant__ LayerParams p) {
+  extern __shared__ __align__(1024) unsigned char smem[];
+  __shared__ __align__(8) unsigned long long bars[2 * kMaxStages + 4];
+  __shared__ uint32_t tmem_base_shared;
+  __shared__ int warp_tot[2][kThreads / 32];
+  __shared__ int last_shared, failed_shared, stopped_shared;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, cta = blockIdx.x;
+  const int A = p.tokens * p.k, N = p.instances;
+  if (smem_u32(smem) & 1023) {   // the swizzled operands need it; the same in every CTA
+    if (cta == 0 && tid == 0) atomicOr(p.control + C_STATUS, TOPOEP_FLAG_INTERNAL);
+    return;
+  }
+
+  // ---- ids by instance; the masks lie in the ring, the tables behind it
+  uint32_t* mask = reinterpret_cast<uint32_t*>(smem);                        // [N][4]
+  uint16_t* slot_of = reinterpret_cast<uint16_t*>(smem + (size_t)16 * N);    // [N]
+  uint16_t* act = reinterpret_cast<uint16_t*>(smem + p.o_act);
+  uint16_t* off = reinterpret_cast<uint16_t*>(smem + p.o_off);
+  uint8_t* tok = smem + p.o_tok;
+  uint16_t* pos = reinterpret_cast<uint16_t*>(smem + p.o_pos);
+  uint16_t* aslot = reinterpret_cast<uint16_t*>(smem + p.o_slot);
+  for (int i = tid; i < N; i += kThreads) reinterpret_cast<uint4*>(mask)[i] = make_uint4(0, 0, 0, 0);
+  if (tid == 0) {
+    for (int s = 0; s < p.stages; ++s) {
+      mbar_init(smem_u32(&bars[s]), 2);                     // full: weights and rows
+      mbar_init(smem_u32(&bars[kMaxStages + s]), 1);        // empty: the products that read it
+    }
+    for (int b = 0; b < 2; ++b) {
+      mbar_init(smem_u32(&bars[2 * kMaxStages + b]), 1);    // accumulator ready
+      mbar_init(smem_u32(&bars[2 * kMaxStages + 2 + b]), 128);   // accumulator read
+    }
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    failed_shared = 0;
+    stopped_shared = 0;
+  }
+  if (warp == 2) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_base_shared)),
+                 "r"(p.tmem_cols) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+  }
+  __syncthreads();
+  for (int a = tid; a < A; a += kThreads) {
+    const int id = p.ids[a];
+    if (id >= 0 && id < N) {
+      const int t = a / p.k;
+      atomicOr(&mask[id * 4 + (t >> 5)], 1u << (t & 31));
+    } else if (id != -1 && cta == 0) {
+      atomicOr(p.control + C_STATUS, TOPOEP_FLAG_BAD_ID);
+    }
+  }
+  __syncthreads();
+  const int per = (N + kThreads - 1) / kThreads, first = min(N, tid * per), last = min(N, first + per);
+  int my_slots = 0, my_rows = 0;
+  for (int i = first; i < last; ++i) {
+    const uint4 m = reinterpret_cast<const uint4*>(mask)[i];
+    const int c = __popc(m.x) + __popc(m.y) + __popc(m.z) + __popc(m.w);
+    my_slots += c > 0;
+    my_rows += c;
+  }
+  int inc_s = my_slots, inc_r = my_rows;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const int a = __shfl_up_sync(0xffffffffu, inc_s, o), b = __shfl_up_sync(0xffffffffu, inc_r, o);
+    if (lane >= o) { inc_s += a; inc_r += b; }
+  }
+  if (lane == 31) { warp_tot[0][warp] = inc_s; warp_tot[1][warp] = inc_r; }
+  __syncthreads();
+  int n_slots = 0, n_rows = 0, s_at = inc_s - my_slots, r_at = inc_r - my_rows;
+#pragma unroll
+  for (int w = 0; w < kThreads / 32; ++w) {
+    if (w < warp) { s_at += warp_tot[0][w]; r_at += warp_tot[1][w]; }
+    n_slots += warp_tot[0][w];
+    n_rows += warp_tot[1][w];
+  }
+  for (int i = first; i < last; ++i) {
+    const uint4 m4 = reinterpret_cast<const uint4*>(mask)[i];
+    const uint32_t m[4] = {m4.x, m4.y, m4.z, m4.w};
+    if (!(m[0] | m[1] | m[2] | m[3])) continue;
+    act[s_at] = (uint16_t)i;
+    off[s_at] = (uint16_t)r_at;
+    slot_of[i] = (uint16_t)s_at++;
+#pragma unroll
+    for (int w = 0; w < 4; ++w)
+      for (uint32_t b = m[w]; b; b &= b - 1) tok[r_at++] = (uint8_t)(w * 32 + __ffs(b) - 1);
+  }
+  if (tid == 0) off[n_slots] = (uint16_t)n_rows;
+  __syncthreads();
+  for (int a = tid; a < A; a += kThreads) {
+    const int id = p.ids[a];
+    uint16_t row = 0xffff, sl = 0;
+    if (id >= 0 && id < N) {
+      const int t = a / p.k;
+      const uint32_t* m = mask + id * 4;
+      int before = __popc(m[t >> 5] & ((1u << (t & 31)) - 1));
+      for (int w = 0; w < (t >> 5); ++w) before += __popc(m[w]);
+      sl = slot_of[id];
+      row = (uint16_t)(off[sl] + before);
+    }
+    pos[a] = row;
+    aslot[a] = sl;
+  }
+  // the ring's bytes were touched by ordinary accesses; the copy unit writes them next
+  asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+  asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+  __syncthreads();
+  asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+  const uint32_t tmem = tmem_base_shared;
+  const uint32_t ring = smem_u32(smem), full = smem_u32(&bars[0]), empty = smem_u32(&bars[kMaxStages]);
+  const uint32_t acc_full = smem_u32(&bars[2 * kMaxStages]), acc_empty = acc_full + 16;
+  const int per_rank = p.e_loc + p.slots;
+  const Runs runs1(n_slots, (p.F + kTileM - 1) / kTileM, (p.H + kStepK - 1) / kStepK);
+  const Runs runs2(n_slots, (p.H + 2 * kTileM - 1) / (2 * kTileM), (p.F + kStepK - 1) / kStepK);
+  volatile int *failed = &failed_shared, *stopped = &stopped_shared;
+
+  if (warp == 0) {
+    if (lane == 0) {   // ---- weights
+      int st = 0;
+      uint32_t ph = 0;
+      bool ok = true;
+      for (int phase = 0; phase < 2 && ok; ++phase) {
+        const Runs& runs = phase ? runs2 : runs1;
+        PieceWalk walk(runs, cta);
+        Piece pc;
+        while (ok && walk.next(pc)) {
+          const int inst = act[pc.slot], r = inst / per_rank, l = inst - r * per_rank;
+          const bool in_main = l < p.e_loc;
+          const int z = in_main ? r * p.e_loc + l : r * p.slots + l - p.e_loc;
+          const CUtensorMap* map = phase ? (in_main ? &maps.main_down : &maps.replica_down)
+                                         : (in_main ? &maps.main_gu : &maps.replica_gu);
+          const int y0 = phase ? pc.m * 2 * kTileM : pc.m * kTileM;
+          const int y1 = phase ? y0 + kTileM : p.F + y0;
+          for (int s = pc.k0; s < pc.k1; ++s) {
+            if (!mbar_wait(empty + 8 * st, ph ^ 1)) { ok = false; break; }
+            const uint32_t dst = ring + st * p.stage_bytes;
+            mbar_expect(full + 8 * st, kStageA);
+            tma_weights(dst, map, s * kStepK, y0, z, full + 8 * st);
+            tma_weights(dst + kHalfBytes, map, s * kStepK, y1, z, full + 8 * st);
+            if (++st == p.stages) { st = 0; ph ^= 1; }
+          }
+        }
+      }
+      if (!ok) *failed = 1;
+    }
+    __syncwarp();
+  } else if (warp == 1) {   // ---- rows of x, then of h
+    int st = 0;
+    uint32_t ph = 0;
+    bool ok = true;
+    for (int phase = 0; phase < 2 && ok; ++phase) {
+      const Runs& runs = phase ? runs2 : runs1;
+      PieceWalk walk(runs, cta);
+      Piece pc;
+      bool waited = phase == 0;
+      while (ok && walk.next(pc)) {
+        if (!waited) {   // every tile of h is written
+          int good = 1;
+          if (lane == 0) good = spin_until(p.control + C_TILES, (unsigned)runs1.tiles);
+          ok = __shfl_sync(0xffffffffu, good, 0) != 0;
+          if (!ok) break;
+          __syncwarp();
+          asm volatile("fence.proxy.async.global;" ::: "memory");
+          waited = true;
+        }
+        const int o = off[pc.slot], n = off[pc.slot + 1] - o, groups = (n + 3) >> 2;
+        int row[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int at = o + min(4 * lane + i, n - 1);
+          row[i] = phase ? at : tok[at];
+        }
+        for (int s = pc.k0; s < pc.k1; ++s) {
+          int good = 1;
+          if (lane == 0) {
+            good = mbar_wait(empty + 8 * st, ph ^ 1);
+            if (good) mbar_expect(full + 8 * st, groups * 512 * (phase + 1));
+          }
+          ok = __shfl_sync(0xffffffffu, good, 0) != 0;
+          if (!ok) break;
+          if (lane < groups) {
+            const uint32_t dst = ring + st * p.stage_bytes + kStageA + lane * 512;
+            if (phase == 0) {
+              tma_rows(dst, &maps.x, s * kStepK, row[0], row[1], row[2], row[3], full + 8 * st);
+            } else {
+              tma_rows(dst, &maps.h, s * kStepK, row[0], row[1], row[2], row[3], full + 8 * st);
+              tma_rows(dst + p.b_half, &maps.h, s * kStepK, p.max_rows + row[0], p.max_rows + row[1],
+                       p.max_rows + row[2], p.max_rows + row[3], full + 8 * st);
+            }
+          }
+          if (++st == p.stages) { st = 0; ph ^= 1; }
+        }
+      }
+    }
+    if (!ok && lane == 0) *failed = 1;
+    __syncwarp();
+  } else if (warp == 2) {
+    if (lane == 0) {   // ---- products
+      int st = 0, buf = 0;
+      uint32_t ph = 0, accph = 0;
+      bool ok = true;
+      for (int phase = 0; phase < 2 && ok; ++phase) {
+        const Runs& runs = phase ? runs2 : runs1;
+        PieceWalk walk(runs, cta);
+        Piece pc;
+        while (ok && walk.next(pc)) {
+          const int n = off[pc.slot + 1] - off[pc.slot], cols = (n + 15) & ~15;
+          const uint32_t idesc = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(cols >> 3) << 17) |
+                                 ((uint32_t)(kTileM >> 4) << 24);
+          if (!mbar_wait(acc_empty + 8 * buf, accph ^ 1)) { ok = false; break; }
+          asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+          const uint32_t d0 = tmem + buf * 2 * p.acc_cols, d1 = d0 + p.acc_cols;
+          for (int s = pc.k0; s < pc.k1; ++s) {
+            if (!mbar_wait(full + 8 * st, ph)) { ok = false; break; }
+            asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+            const uint32_t base = ring + st * p.stage_bytes;
+            const uint64_t a0 = operand(base), a1 = operand(base + kHalfBytes);
+            const uint64_t b0 = operand(base + kStageA), b1 = operand(base + kStageA + p.b_half);
+#pragma unroll
+            for (int j = 0; j < kStepK / 16; ++j) {   // 16 elements of the sum are 32 bytes
+              const uint32_t add = s > pc.k0 || j > 0;
+              mma(d0, a0 + 2 * j, b0 + 2 * j, idesc, add);
+              mma(d1, a1 + 2 * j, b0 + 2 * j, idesc, add);
+              if (phase) {
+                mma(d0, a0 + 2 * j, b1 + 2 * j, idesc, 1);
+                mma(d1, a1 + 2 * j, b1 + 2 * j, idesc, 1);
+              }
+            }
+            mma_commit(empty + 8 * st);
+            if (++st == p.stages) { st = 0; ph ^= 1; }
+          }
+          if (!ok) break;
+          mma_commit(acc_full + 8 * buf);
+          buf ^= 1;
+          if (buf == 0) accph ^= 1;
+        }
+      }
+      if (!ok) *failed = 1;
+    }
+    __syncwarp();
+  } else if (warp >= 4) {   // ---- accumulators
+    const int quad = warp & 3, row = quad * 32 + lane, etid = tid - 128;
+    int buf = 0;
+    uint32_t accph = 0;
+    bool ok = true;
+    for (int phase = 0; phase < 2 && ok; ++phase) {
+      const Runs& runs = phase ? runs2 : runs1;
+      PieceWalk walk(runs, cta);
+      Piece pc;
+      while (walk.next(pc)) {
+        if (!mbar_wait(acc_full + 8 * buf, accph)) *stopped = 1;
+        epilogue_sync();   // the four warps go on, or stop, together
+        if (*stopped) { ok = false; break; }
+        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+        const int o = off[pc.slot], n = off[pc.slot + 1] - o;
+        const uint32_t d = tmem + buf * 2 * p.acc_cols + ((uint32_t)quad << 21);
+        const bool whole = pc.k0 == 0 && pc.k1 == runs.steps;
+        float* part = p.partial + (size_t)(cta * 2 + (pc.k0 > 0 ? 0 : 1)) * p.acc_cols * 256 + row;
+        const int f = pc.m * kTileM + row;
+        const int c0 = runs.cta_of(pc.tile * runs.steps);
+        float* yp = p.yp + ((size_t)(cta - c0) * n_rows + o) * p.H + pc.m * 2 * kTileM + row;
+        const bool in0 = pc.m * 2 * kTileM + row < p.H, in1 = pc.m * 2 * kTileM + kTileM + row < p.H;
+        for (int c = 0; c < n; c += 16) {
+          float g[16], u[16];
+          tmem_load16(d + c, g);
+          tmem_load16(d + p.acc_cols + c, u);
+          asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+          if (phase) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i)
+              if (c + i < n) {
+                if (in0) yp[(size_t)(c + i) * p.H] = g[i];
+                if (in1) yp[(size_t)(c + i) * p.H + kTileM] = u[i];
+              }
+          } else if (whole) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i)
+              if (c + i < n && f < p.F) store_h(p, o + c + i, f, g[i], u[i]);
+          } else {
+#pragma unroll
+            for (int i = 0; i < 16; ++i)
+              if (c + i < n) {
+                __stcg(part + (c + i) * 256, g[i]);
+                __stcg(part + (c + i) * 256 + kTileM, u[i]);
+              }
+          }
+        }
+        asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+        mbar_arrive(acc_empty + 8 * buf);
+        buf ^= 1;
+        if (buf == 0) accph ^= 1;
+        if (phase) continue;
+        if (!whole) {   // the last CTA of the tile sums the parts, in the order of the CTAs
+          __threadfence();
+          epilogue_sync();
+          if (etid == 0) {
+            const unsigned mine = pc.k1 - pc.k0;
+            const unsigned before = atomicAdd(p.tile_steps + pc.tile, mine);
+            last_shared = before + mine == (unsigned)runs.steps;
+            if (last_shared) p.tile_steps[pc.tile] = 0;   // ready for the next call
+            __threadfence();
+          }
+          epilogue_sync();
+          if (!last_shared) continue;
+          const int first_unit = pc.tile * runs.steps, c1 = runs.cta_of(first_unit + runs.steps - 1);
+          for (int i = 0; i < n; ++i) {
+            float g = 0.0f, u = 0.0f;
+            for (int c = c0; c <= c1; ++c) {
+              const float* from = p.partial + (size_t)(c * 2 + (runs.start(c) > first_unit ? 0 : 1)) * p.acc_cols * 256 +
+                                  i * 256 + row;
+              g += __ldcg(from);
+              u += __ldcg(from + kTileM);
+            }
+            if (f < p.F) store_h(p, o + i, f, g, u);
+          }
+        }
+        // h is read by the copy unit of other CTAs
+        asm volatile("fence.proxy.async.global;" ::: "memory");
+        __threadfence();
+        epilogue_sync();
+        if (etid == 0) add_release(p.control + C_TILES, 1);
+      }
+    }
+    if (!ok) *failed = 1;
+  }
+
+  // ---- all partial results are written: weigh and sum
+  __threadfence();
+  __syncthreads();
+  if (tid == 0) {
+    add_release(p.control + C_ARRIVE, 1);
+    if (!spin_until(p.control + C_ARRIVE, gridDim.x)) failed_shared = 1;
+  }
+  __syncthreads();
+  {
+    const int quads = p.H >> 2, items = p.tokens * quads;
+    for (int it = cta * kThreads + tid; it < items; it += gridDim.x * kThreads) {
+      const int t = it / quads, h0 = (it - t * quads) * 4;
+      float4 sum = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+      for (int j = 0; j < p.k; ++j) {
+        const int a = t * p.k + j;
+        if (pos[a] == 0xffff) continue;
+        const int u0 = (aslot[a] * runs2.per_slot + h0 / (2 * kTileM)) * runs2.steps;
+        const int planes = runs2.cta_of(u0 + runs2.steps - 1) - runs2.cta_of(u0) + 1;
+        float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+        for (int s = 0; s < planes; ++s) {
+          const float4 q = __ldcg(reinterpret_cast<const float4*>(p.yp + ((size_t)s * n_rows + pos[a]) * p.H + h0));
+          v.x += q.x; v.y += q.y; v.z += q.z; v.w += q.w;
+        }
+        const float w = p.weights[a];
+        sum.x += w * v.x; sum.y += w * v.y; sum.z += w * v.z; sum.w += w * v.w;
+      }
+      __nv_bfloat16* y = p.y + t * p.y_stride + h0;
+      const __nv_bfloat162 lo = __floats2bfloat162_rn(sum.x, sum.y), hi = __floats2bfloat162_rn(sum.z, sum.w);
+      if ((reinterpret_cast<uintptr_t>(y) & 7) == 0) {
+        uint2 v;
+        v.x = *reinterpret_cast<const uint32_t*>(&lo);
+        v.y = *reinterpret_cast<const uint32_t*>(&hi);
+        *reinterpret_cast<uint2*>(y) = v;
+      } else {
+        y[0] = lo.x; y[1] = lo.y; y[2] = hi.x; y[3] = hi.y;
+      }
+    }
+  }
+  if (failed_shared) {   // a wait ran out: report it and let the copies in flight land
+    if (tid == 0) {
+      atomicOr(p.control + C_STATUS, TOPOEP_FLAG_INTERNAL);
+      for (int s = 0; s < p.stages; ++s)
+        if (!mbar_wait(full + 8 * s, 0)) mbar_wait(full + 8 * s, 1);
+    }
+    __syncthreads();
+  }
+  if (tid == 0) {   // the last CTA to leave makes the counters ready for the next call
+    const unsigned before = atomicAdd(p.control + C_LEAVE, 1);
+    if (before + 1 == gridDim.x) {
+      p.control[C_TILES] = 0;
+      p.control[C_ARRIVE] = 0;
+      p.control[C_LEAVE] = 0;
+    }
+  }
+  if (warp == 2) {
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(p.tmem_cols) : "memory");
+  }
+}
+
 constexpr size_t kAlign = 256;
 inline size_t align_up(size_t x) { return (x + kAlign - 1) / kAlign * kAlign; }
+
+constexpr int kMaxCtas = 160;              // scratch is laid out for at most so many
+constexpr size_t kSharedLimit = 226 * 1024;
+
+typedef CUresult (*EncodeFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*,
+                             const cuuint64_t*, const cuuint32_t*, const cuuint32_t*,
+                             CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion,
+                             CUtensorMapFloatOOBfill);
+
+EncodeFn encode_fn() {
+  void* fn = nullptr;
+  cudaDriverEntryPointQueryResult found;
+  if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &fn, cudaEnableDefault, &found) != cudaSuccess ||
+      found != cudaDriverEntryPointSuccess)
+    return nullptr;
+  return reinterpret_cast<EncodeFn>(fn);
+}
+
+// bfloat16 map of rank 2 or 3; boxes are 64 elements (one swizzled row) by `box_rows`.
+bool encode(EncodeFn fn, CUtensorMap* map, const void* base, int rank, uint64_t d0, uint64_t d1,
+            uint64_t d2, uint64_t s1_bytes, uint64_t s2_bytes, uint32_t box_rows) {
+  const cuuint64_t dims[3] = {d0, d1, d2}, strides[2] = {s1_bytes, s2_bytes};
+  const cuuint32_t box[3] = {kStepK, box_rows, 1}, step[3] = {1, 1, 1};
+  return fn(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, rank, const_cast<void*>(base), dims, strides, box,
+            step, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+            CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+// CTAs that share a tile of `steps` when `units` are divided over the most CTAs there can be.
+long long planes_of(long long units, long long steps) {
+  const long long q = units / kMaxCtas;
+  return q == 0 ? steps : std::min(steps, (steps + q - 1) / q + 1);
+}
+
+// Shared-memory layout of a call with `tokens` rows; false if a CTA's ring would be too short.
+struct Shape {
+  int cols, b_half, stage_bytes, stages, o_act, o_off, o_tok, o_pos, o_slot;
+  size_t bytes;
+  Shape(int tokens, int k, int instances) {
+    const int a = tokens * k, slots = std::min(a, instances);
+    cols = (tokens + 15) / 16 * 16;
+    b_half = cols * kStepK * 2;
+    stage_bytes = kStageA + 2 * b_half;
+    const size_t tables = 2 * (size_t)slots + 2 * ((size_t)slots + 2) + (a + 1) / 2 * 2 + 4 * (size_t)a + 16;
+    stages = (int)std::min<size_t>(kMaxStages, (kSharedLimit - tables) / stage_bytes);
+    const int ring = stages * stage_bytes;
+    o_act = ring;
+    o_off = o_act + 2 * slots;
+    o_pos = o_off + 2 * (slots + 2);
+    o_slot = o_pos + 2 * a;
+    o_tok = o_slot + 2 * a;
+    bytes = ring + tables;
+  }
+};
 
 }  // namespace
 
@@ -88,12 +713,14 @@ inline size_t align_up(size_t x) { return (x + kAlign - 1) / kAlign * kAlign; }
 using namespace topoep;
 
 struct topoep_experts_ctx {
-  int ranks, e_loc, slots, instances, hidden, ffn, top_k, max_tokens;
+  int ranks, e_loc, slots, instances, hidden, ffn, top_k, max_tokens, max_rows, ctas;
   const void* main;
   const void* replica;
-  bool have_params;
+  bool have_params, tiled;   // tiled: sizes that the copy unit can address
   unsigned char* ws;
-  size_t ws_bytes, off_h;
+  size_t ws_bytes, off_h, off_steps, off_partial, off_yp;
+  EncodeFn encode;
+  Maps maps;
 };
 
 extern "C" int topoep_experts_create(topoep_experts_t* out, int ranks, int experts_per_rank,
@@ -115,8 +742,25 @@ extern "C" int topoep_experts_create(topoep_experts_t* out, int ranks, int exper
   h->ffn = ffn;
   h->top_k = top_k;
   h->max_tokens = max_tokens;
+  h->max_rows = max_tokens * top_k;
+  // rows of both matrices start on 16 bytes, as the copy unit needs them
+  h->tiled = hidden % 8 == 0 && ffn % 8 == 0;
   h->off_h = kAlign;
-  h->ws_bytes = h->off_h + align_up((size_t)4 * max_tokens * top_k * ffn);
+  // h: 32 bits an element, or two bfloat16 parts
+  h->off_steps = h->off_h + align_up((size_t)4 * h->max_rows * ffn);
+  h->off_partial = h->off_yp = h->ws_bytes = h->off_steps;
+  if (h->tiled) {
+    const long long steps = (ffn + kStepK - 1) / kStepK, per_slot = (hidden + 2 * kTileM - 1) / (2 * kTileM);
+    const int most = std::min(h->max_rows, h->instances);
+    long long rows = 0;   // rows of partial results over all planes, at worst
+    for (int n = 1; n <= most; ++n)
+      rows = std::max(rows, planes_of(n * per_slot * steps, steps) *
+                                std::min<long long>(h->max_rows, (long long)n * max_tokens));
+    h->off_partial = h->off_steps + align_up((size_t)4 * most * ((ffn + kTileM - 1) / kTileM));
+    const size_t cols = (max_tokens + 15) / 16 * 16;
+    h->off_yp = h->off_partial + align_up((size_t)kMaxCtas * 2 * cols * 2 * kTileM * 4);
+    h->ws_bytes = h->off_yp + align_up((size_t)4 * rows * hidden);
+  }
   *out = h;
   return TOPOEP_OK;
 }
@@ -129,10 +773,25 @@ extern "C" int topoep_experts_set_workspace(topoep_experts_t h, void* dev_ptr, s
   if (!h || !dev_ptr) return TOPOEP_ERR_NULL;
   if (bytes < h->ws_bytes || !aligned_to(dev_ptr, kAlign)) return TOPOEP_ERR_WORKSPACE;
   h->ws = nullptr;
-  cudaError_t e = cudaMemset(dev_ptr, 0, kAlign);
+  unsigned char* ws = static_cast<unsigned char*>(dev_ptr);
+  cudaError_t e = cudaMemset(ws, 0, kAlign);
+  if (e == cudaSuccess && h->tiled) {
+    int dev = 0, sms = 0;
+    e = cudaGetDevice(&dev);
+    if (e == cudaSuccess) e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
+    h->ctas = std::min(sms, kMaxCtas);
+    if (e == cudaSuccess) e = cudaMemset(ws + h->off_steps, 0, h->off_partial - h->off_steps);
+    if (e == cudaSuccess)
+      e = cudaFuncSetAttribute(experts_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSharedLimit);
+    if (e != cudaSuccess) return TOPOEP_ERR_CUDA;
+    h->encode = encode_fn();
+    if (!h->encode || !encode(h->encode, &h->maps.h, ws + h->off_h, 2, h->ffn, 2 * h->max_rows, 1,
+                              2 * (uint64_t)h->ffn, 0, 1))
+      return TOPOEP_ERR_CUDA;
+  }
   if (e == cudaSuccess) e = cudaDeviceSynchronize();
   if (e != cudaSuccess) return TOPOEP_ERR_CUDA;
-  h->ws = static_cast<unsigned char*>(dev_ptr);
+  h->ws = ws;
   return TOPOEP_OK;
 }
 
@@ -141,11 +800,75 @@ extern "C" int topoep_experts_set_params(topoep_experts_t h, const void* dev_mai
   if (!h) return TOPOEP_ERR_NULL;
   if ((h->e_loc > 0 && !dev_main_params) || (h->slots > 0 && !dev_replica_buf)) return TOPOEP_ERR_NULL;
   if (!aligned_to(dev_main_params, 16) || !aligned_to(dev_replica_buf, 16)) return TOPOEP_ERR_ALIGN;
+  if (h->tiled) {
+    const EncodeFn fn = encode_fn();
+    if (!fn) return TOPOEP_ERR_CUDA;
+    const uint64_t H = h->hidden, F = h->ffn, W = 6 * H * F;
+    for (int i = 0; i < 2; ++i) {
+      const uint64_t n = (uint64_t)h->ranks * (i ? h->slots : h->e_loc);
+      const char* base = static_cast<const char*>(i ? dev_replica_buf : dev_main_params);
+      if (n == 0) continue;
+      if (!encode(fn, i ? &h->maps.replica_gu : &h->maps.main_gu, base, 3, H, 2 * F, n, 2 * H, W, kTileM) ||
+          !encode(fn, i ? &h->maps.replica_down : &h->maps.main_down, base + 4 * H * F, 3, F, H, n, 2 * F, W, kTileM))
+        return TOPOEP_ERR_CUDA;
+    }
+  }
   h->main = dev_main_params;
   h->replica = dev_replica_buf;
   h->have_params = true;
   return TOPOEP_OK;
 }
+
+namespace {
+
+cudaError_t launch_tiled(topoep_experts_t h, const ExpertsParams& a, cudaStream_t stream) {
+  Maps maps = h->maps;
+  const uint64_t stride = a.tokens > 1 ? 2 * (uint64_t)a.x_stride : 2 * (uint64_t)h->hidden;
+  if (!encode(h->encode, &maps.x, a.x, 2, h->hidden, a.tokens, 1, stride, 0, 1)) return cudaErrorInvalidValue;
+  const Shape sh(a.tokens, a.k, h->instances);
+  LayerParams p = {};
+  p.ids = a.ids;
+  p.weights = a.weights;
+  p.y = a.y;
+  p.control = reinterpret_cast<uint32_t*>(h->ws);
+  p.tile_steps = reinterpret_cast<unsigned*>(h->ws + h->off_steps);
+  p.partial = reinterpret_cast<float*>(h->ws + h->off_partial);
+  p.h = reinterpret_cast<__nv_bfloat16*>(h->ws + h->off_h);
+  p.yp = reinterpret_cast<float*>(h->ws + h->off_yp);
+  p.y_stride = a.y_stride;
+  p.tokens = a.tokens;
+  p.k = a.k;
+  p.H = a.H;
+  p.F = a.F;
+  p.e_loc = a.e_loc;
+  p.slots = a.slots;
+  p.instances = a.instances;
+  p.max_rows = h->max_rows;
+  p.stages = sh.stages;
+  p.stage_bytes = sh.stage_bytes;
+  p.b_half = sh.b_half;
+  p.acc_cols = sh.cols;
+  p.tmem_cols = 32;
+  while (p.tmem_cols < 4 * sh.cols) p.tmem_cols *= 2;
+  p.o_act = sh.o_act;
+  p.o_off = sh.o_off;
+  p.o_tok = sh.o_tok;
+  p.o_pos = sh.o_pos;
+  p.o_slot = sh.o_slot;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(h->ctas);
+  cfg.blockDim = dim3(kThreads);
+  cfg.dynamicSmemBytes = sh.bytes;
+  cfg.stream = stream;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeCooperative;
+  attr[0].val.cooperative = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, experts_kernel, maps, p);
+}
+
+}  // namespace
 
 extern "C" int topoep_experts_forward(topoep_experts_t h, const void* dev_x, int64_t x_row_stride,
                                       const int32_t* dev_ids, const float* dev_weights, int tokens,
@@ -179,10 +902,16 @@ extern "C" int topoep_experts_forward(topoep_experts_t h, const void* dev_x, int
   p.e_loc = h->e_loc;
   p.slots = h->slots;
   p.instances = h->instances;
-  const int per = kAnyThreads / 32;
-  experts_gate_any_kernel<<<dim3((p.F + per - 1) / per, tokens * p.k), kAnyThreads, 0, st>>>(p);
-  experts_down_any_kernel<<<dim3((p.H + per - 1) / per, tokens), kAnyThreads, 0, st>>>(p);
-  return cudaGetLastError() == cudaSuccess ? TOPOEP_OK : TOPOEP_ERR_CUDA;
+  cudaError_t e;
+  if (h->tiled && aligned_to(dev_x, 16) && (tokens == 1 || x_row_stride % 8 == 0)) {
+    e = launch_tiled(h, p, st);
+  } else {
+    const int per = kAnyThreads / 32;
+    experts_gate_any_kernel<<<dim3((p.F + per - 1) / per, tokens * p.k), kAnyThreads, 0, st>>>(p);
+    experts_down_any_kernel<<<dim3((p.H + per - 1) / per, tokens), kAnyThreads, 0, st>>>(p);
+    e = cudaGetLastError();
+  }
+  return e == cudaSuccess ? TOPOEP_OK : TOPOEP_ERR_CUDA;
 }
 
 extern "C" int topoep_experts_read_status(topoep_experts_t h, uint32_t* host_flags) {

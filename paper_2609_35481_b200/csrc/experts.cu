@@ -134,8 +134,7 @@ struct LayerParams {
   float* yp;                 // [plane][row][H]
   long long y_stride;
   int tokens, k, H, F, e_loc, slots, instances, max_rows;
-  int stages, stage_bytes, b_half;   // b_half: bytes of the columns' side (one part)
-  int tmem_cols, acc_cols;
+  int ring_bytes, tmem_cols, acc_cols;
   int o_act, o_off, o_tok, o_pos, o_slot;   // offsets of the tables behind the ring
 };
 
@@ -173,6 +172,11 @@ __device__ __forceinline__ void tma_rows(uint32_t dst, const CUtensorMap* map, i
       "cp.async.bulk.tensor.2d.shared::cluster.global.tile::gather4.mbarrier::complete_tx::bytes "
       "[%0], [%1, {%2, %3, %4, %5, %6}], [%7];"
       ::"r"(dst), "l"(map), "r"(x), "r"(r0), "r"(r1), "r"(r2), "r"(r3), "r"(bar) : "memory");
+}
+__device__ __forceinline__ void tma_box(uint32_t dst, const CUtensorMap* map, int x, int y, uint32_t bar) {
+  asm volatile(
+      "cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];"
+      ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(bar) : "memory");
 }
 // Shared-memory operand: K-major rows of 128 bytes in the 128-byte swizzle, 8-row groups 1024 apart.
 __device__ __forceinline__ uint64_t operand(uint32_t addr) {
@@ -270,7 +274,7 @@ experts_kernel(const __grid_constant__ Maps maps, const __grid_constant__ LayerP
   extern __shared__ __align__(1024) unsigned char smem[];
   __shared__ __align__(8) unsigned long long bars[2 * kMaxStages + 4];
   __shared__ uint32_t tmem_base_shared;
-  __shared__ int warp_tot[2][kThreads / 32];
+  __shared__ int warp_tot[3][kThreads / 32];
   __shared__ int last_shared, failed_shared, stopped_shared;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, cta = blockIdx.x;
   const int A = p.tokens * p.k, N = p.instances;
@@ -289,7 +293,7 @@ experts_kernel(const __grid_constant__ Maps maps, const __grid_constant__ LayerP
   uint16_t* aslot = reinterpret_cast<uint16_t*>(smem + p.o_slot);
   for (int i = tid; i < N; i += kThreads) reinterpret_cast<uint4*>(mask)[i] = make_uint4(0, 0, 0, 0);
   if (tid == 0) {
-    for (int s = 0; s < p.stages; ++s) {
+    for (int s = 0; s < kMaxStages; ++s) {
       mbar_init(smem_u32(&bars[s]), 2);                     // full: weights and rows
       mbar_init(smem_u32(&bars[kMaxStages + s]), 1);        // empty: the products that read it
     }
@@ -318,27 +322,30 @@ experts_kernel(const __grid_constant__ Maps maps, const __grid_constant__ LayerP
   }
   __syncthreads();
   const int per = (N + kThreads - 1) / kThreads, first = min(N, tid * per), last = min(N, first + per);
-  int my_slots = 0, my_rows = 0;
+  int my_slots = 0, my_rows = 0, my_most = 0;
   for (int i = first; i < last; ++i) {
     const uint4 m = reinterpret_cast<const uint4*>(mask)[i];
     const int c = __popc(m.x) + __popc(m.y) + __popc(m.z) + __popc(m.w);
     my_slots += c > 0;
     my_rows += c;
+    my_most = max(my_most, c);
   }
+  my_most = __reduce_max_sync(0xffffffffu, my_most);
   int inc_s = my_slots, inc_r = my_rows;
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1) {
     const int a = __shfl_up_sync(0xffffffffu, inc_s, o), b = __shfl_up_sync(0xffffffffu, inc_r, o);
     if (lane >= o) { inc_s += a; inc_r += b; }
   }
-  if (lane == 31) { warp_tot[0][warp] = inc_s; warp_tot[1][warp] = inc_r; }
+  if (lane == 31) { warp_tot[0][warp] = inc_s; warp_tot[1][warp] = inc_r; warp_tot[2][warp] = my_most; }
   __syncthreads();
-  int n_slots = 0, n_rows = 0, s_at = inc_s - my_slots, r_at = inc_r - my_rows;
+  int n_slots = 0, n_rows = 0, most = 0, s_at = inc_s - my_slots, r_at = inc_r - my_rows;
 #pragma unroll
   for (int w = 0; w < kThreads / 32; ++w) {
     if (w < warp) { s_at += warp_tot[0][w]; r_at += warp_tot[1][w]; }
     n_slots += warp_tot[0][w];
     n_rows += warp_tot[1][w];
+    most = max(most, warp_tot[2][w]);
   }
   for (int i = first; i < last; ++i) {
     const uint4 m4 = reinterpret_cast<const uint4*>(mask)[i];
@@ -373,6 +380,9 @@ experts_kernel(const __grid_constant__ Maps maps, const __grid_constant__ LayerP
   __syncthreads();
   asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
   const uint32_t tmem = tmem_base_shared;
+  // a stage holds the weights of a step and the rows of the fullest instance, in both parts
+  const int b_half = ((most + 15) & ~15) * kStepK * 2, stage_bytes = kStageA + 2 * b_half;
+  const int stages = min(kMaxStages, p.ring_bytes / stage_bytes);
   const uint32_t ring = smem_u32(smem), full = smem_u32(&bars[0]), empty = smem_u32(&bars[kMaxStages]);
   const uint32_t acc_full = smem_u32(&bars[2 * kMaxStages]), acc_empty = acc_full + 16;
   const int per_rank = p.e_loc + p.slots;
@@ -399,11 +409,11 @@ experts_kernel(const __grid_constant__ Maps maps, const __grid_constant__ LayerP
           const int y1 = phase ? y0 + kTileM : p.F + y0;
           for (int s = pc.k0; s < pc.k1; ++s) {
             if (!mbar_wait(empty + 8 * st, ph ^ 1)) { ok = false; break; }
-            const uint32_t dst = ring + st * p.stage_bytes;
+            const uint32_t dst = ring + st * stage_bytes;
             mbar_expect(full + 8 * st, kStageA);
             tma_weights(dst, map, s * kStepK, y0, z, full + 8 * st);
             tma_weights(dst + kHalfBytes, map, s * kStepK, y1, z, full + 8 * st);
-            if (++st == p.stages) { st = 0; ph ^= 1; }
+            if (++st == stages) { st = 0; ph ^= 1; }
           }
         }
       }
@@ -429,32 +439,32 @@ experts_kernel(const __grid_constant__ Maps maps, const __grid_constant__ LayerP
           asm volatile("fence.proxy.async.global;" ::: "memory");
           waited = true;
         }
-        const int o = off[pc.slot], n = off[pc.slot + 1] - o, groups = (n + 3) >> 2;
+        // x: four gathered rows a lane; h: 16 adjacent rows a lane, the first lanes the rounded
+        // values and the next ones the rests.  Rows past the instance's last are some other row's:
+        // columns of the product that nobody reads.
+        const int o = off[pc.slot], n = off[pc.slot + 1] - o;
+        const int groups = phase ? (n + 15) >> 4 : (n + 3) >> 2;
+        const int copies = phase ? 2 * groups : groups, bytes = phase ? 2 * groups * 2048 : groups * 512;
         int row[4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const int at = o + min(4 * lane + i, n - 1);
-          row[i] = phase ? at : tok[at];
-        }
+        for (int i = 0; i < 4; ++i) row[i] = tok[o + min(4 * lane + i, n - 1)];
+        const bool rest = lane >= groups;
+        const int y = o + 16 * (rest ? lane - groups : lane) + (rest ? p.max_rows : 0);
+        const uint32_t to = phase ? (rest ? b_half + (lane - groups) * 2048 : lane * 2048) : lane * 512;
         for (int s = pc.k0; s < pc.k1; ++s) {
           int good = 1;
           if (lane == 0) {
             good = mbar_wait(empty + 8 * st, ph ^ 1);
-            if (good) mbar_expect(full + 8 * st, groups * 512 * (phase + 1));
+            if (good) mbar_expect(full + 8 * st, bytes);
           }
           ok = __shfl_sync(0xffffffffu, good, 0) != 0;
           if (!ok) break;
-          if (lane < groups) {
-            const uint32_t dst = ring + st * p.stage_bytes + kStageA + lane * 512;
-            if (phase == 0) {
-              tma_rows(dst, &maps.x, s * kStepK, row[0], row[1], row[2], row[3], full + 8 * st);
-            } else {
-              tma_rows(dst, &maps.h, s * kStepK, row[0], row[1], row[2], row[3], full + 8 * st);
-              tma_rows(dst + p.b_half, &maps.h, s * kStepK, p.max_rows + row[0], p.max_rows + row[1],
-                       p.max_rows + row[2], p.max_rows + row[3], full + 8 * st);
-            }
+          if (lane < copies) {
+            const uint32_t dst = ring + st * stage_bytes + kStageA + to;
+            if (phase == 0) tma_rows(dst, &maps.x, s * kStepK, row[0], row[1], row[2], row[3], full + 8 * st);
+            else tma_box(dst, &maps.h, s * kStepK, y, full + 8 * st);
           }
-          if (++st == p.stages) { st = 0; ph ^= 1; }
+          if (++st == stages) { st = 0; ph ^= 1; }
         }
       }
     }
@@ -479,9 +489,9 @@ experts_kernel(const __grid_constant__ Maps maps, const __grid_constant__ LayerP
           for (int s = pc.k0; s < pc.k1; ++s) {
             if (!mbar_wait(full + 8 * st, ph)) { ok = false; break; }
             asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-            const uint32_t base = ring + st * p.stage_bytes;
+            const uint32_t base = ring + st * stage_bytes;
             const uint64_t a0 = operand(base), a1 = operand(base + kHalfBytes);
-            const uint64_t b0 = operand(base + kStageA), b1 = operand(base + kStageA + p.b_half);
+            const uint64_t b0 = operand(base + kStageA), b1 = operand(base + kStageA + b_half);
 #pragma unroll
             for (int j = 0; j < kStepK / 16; ++j) {   // 16 elements of the sum are 32 bytes
               const uint32_t add = s > pc.k0 || j > 0;
@@ -493,7 +503,7 @@ experts_kernel(const __grid_constant__ Maps maps, const __grid_constant__ LayerP
               }
             }
             mma_commit(empty + 8 * st);
-            if (++st == p.stages) { st = 0; ph ^= 1; }
+            if (++st == stages) { st = 0; ph ^= 1; }
           }
           if (!ok) break;
           mma_commit(acc_full + 8 * buf);
@@ -631,7 +641,7 @@ experts_kernel(const __grid_constant__ Maps maps, const __grid_constant__ LayerP
   if (failed_shared) {   // a wait ran out: report it and let the copies in flight land
     if (tid == 0) {
       atomicOr(p.control + C_STATUS, TOPOEP_FLAG_INTERNAL);
-      for (int s = 0; s < p.stages; ++s)
+      for (int s = 0; s < stages; ++s)
         if (!mbar_wait(full + 8 * s, 0)) mbar_wait(full + 8 * s, 1);
     }
     __syncthreads();
@@ -685,18 +695,14 @@ long long planes_of(long long units, long long steps) {
   return q == 0 ? steps : std::min(steps, (steps + q - 1) / q + 1);
 }
 
-// Shared-memory layout of a call with `tokens` rows; false if a CTA's ring would be too short.
+// Shared memory of a call: the ring, cut into stages on the device, and the tables behind it.
 struct Shape {
-  int cols, b_half, stage_bytes, stages, o_act, o_off, o_tok, o_pos, o_slot;
+  int ring, o_act, o_off, o_tok, o_pos, o_slot;
   size_t bytes;
   Shape(int tokens, int k, int instances) {
     const int a = tokens * k, slots = std::min(a, instances);
-    cols = (tokens + 15) / 16 * 16;
-    b_half = cols * kStepK * 2;
-    stage_bytes = kStageA + 2 * b_half;
     const size_t tables = 2 * (size_t)slots + 2 * ((size_t)slots + 2) + (a + 1) / 2 * 2 + 4 * (size_t)a + 16;
-    stages = (int)std::min<size_t>(kMaxStages, (kSharedLimit - tables) / stage_bytes);
-    const int ring = stages * stage_bytes;
+    ring = (int)((kSharedLimit - tables) / 1024 * 1024);
     o_act = ring;
     o_off = o_act + 2 * slots;
     o_pos = o_off + 2 * (slots + 2);
@@ -786,7 +792,7 @@ extern "C" int topoep_experts_set_workspace(topoep_experts_t h, void* dev_ptr, s
     if (e != cudaSuccess) return TOPOEP_ERR_CUDA;
     h->encode = encode_fn();
     if (!h->encode || !encode(h->encode, &h->maps.h, ws + h->off_h, 2, h->ffn, 2 * h->max_rows, 1,
-                              2 * (uint64_t)h->ffn, 0, 1))
+                              2 * (uint64_t)h->ffn, 0, 16))
       return TOPOEP_ERR_CUDA;
   }
   if (e == cudaSuccess) e = cudaDeviceSynchronize();
@@ -844,12 +850,10 @@ cudaError_t launch_tiled(topoep_experts_t h, const ExpertsParams& a, cudaStream_
   p.slots = a.slots;
   p.instances = a.instances;
   p.max_rows = h->max_rows;
-  p.stages = sh.stages;
-  p.stage_bytes = sh.stage_bytes;
-  p.b_half = sh.b_half;
-  p.acc_cols = sh.cols;
+  p.ring_bytes = sh.ring;
+  p.acc_cols = (a.tokens + 15) / 16 * 16;
   p.tmem_cols = 32;
-  while (p.tmem_cols < 4 * sh.cols) p.tmem_cols *= 2;
+  while (p.tmem_cols < 4 * p.acc_cols) p.tmem_cols *= 2;
   p.o_act = sh.o_act;
   p.o_off = sh.o_off;
   p.o_tok = sh.o_tok;

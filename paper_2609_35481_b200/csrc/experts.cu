@@ -349,14 +349,12 @@ experts_kernel(const __grid_constant__ Maps maps, const __grid_constant__ LayerP
   }
   for (int i = first; i < last; ++i) {
     const uint4 m4 = reinterpret_cast<const uint4*>(mask)[i];
-    const uint32_t m[4] = {m4.x, m4.y, m4.z, m4.w};
-    if (!(m[0] | m[1] | m[2] | m[3])) continue;
+    const int c = __popc(m4.x) + __popc(m4.y) + __popc(m4.z) + __popc(m4.w);
+    if (c == 0) continue;
     act[s_at] = (uint16_t)i;
     off[s_at] = (uint16_t)r_at;
     slot_of[i] = (uint16_t)s_at++;
-#pragma unroll
-    for (int w = 0; w < 4; ++w)
-      for (uint32_t b = m[w]; b; b &= b - 1) tok[r_at++] = (uint8_t)(w * 32 + __ffs(b) - 1);
+    r_at += c;
   }
   if (tid == 0) off[n_slots] = (uint16_t)n_rows;
   __syncthreads();
@@ -370,6 +368,7 @@ experts_kernel(const __grid_constant__ Maps maps, const __grid_constant__ LayerP
       for (int w = 0; w < (t >> 5); ++w) before += __popc(m[w]);
       sl = slot_of[id];
       row = (uint16_t)(off[sl] + before);
+      tok[row] = (uint8_t)t;
     }
     pos[a] = row;
     aslot[a] = sl;
@@ -525,71 +524,99 @@ experts_kernel(const __grid_constant__ Maps maps, const __grid_constant__ LayerP
       Piece pc;
       while (walk.next(pc)) {
         if (!mbar_wait(acc_full + 8 * buf, accph)) *stopped = 1;
+        const int first_unit = pc.tile * runs.steps;
+        const bool whole = pc.k0 == 0 && pc.k1 == runs.steps;
+        if (phase == 0 && !whole && etid == 0)   // the other parts of the tile may be there already
+          last_shared = load_acquire(p.tile_steps + pc.tile) == (unsigned)(runs.steps - pc.k1 + pc.k0);
         epilogue_sync();   // the four warps go on, or stop, together
         if (*stopped) { ok = false; break; }
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
         const int o = off[pc.slot], n = off[pc.slot + 1] - o;
+        const int c0 = runs.cta_of(first_unit);
         const uint32_t d = tmem + buf * 2 * p.acc_cols + ((uint32_t)quad << 21);
-        const bool whole = pc.k0 == 0 && pc.k1 == runs.steps;
-        float* part = p.partial + (size_t)(cta * 2 + (pc.k0 > 0 ? 0 : 1)) * p.acc_cols * 256 + row;
-        const int f = pc.m * kTileM + row;
-        const int c0 = runs.cta_of(pc.tile * runs.steps);
-        float* yp = p.yp + ((size_t)(cta - c0) * n_rows + o) * p.H + pc.m * 2 * kTileM + row;
-        const bool in0 = pc.m * 2 * kTileM + row < p.H, in1 = pc.m * 2 * kTileM + kTileM + row < p.H;
-        for (int c = 0; c < n; c += 16) {
-          float g[16], u[16];
-          tmem_load16(d + c, g);
-          tmem_load16(d + p.acc_cols + c, u);
-          asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
-          if (phase) {
+        bool finish = false;
+        if (phase) {
+          float* yp = p.yp + ((size_t)(cta - c0) * n_rows + o) * p.H + pc.m * 2 * kTileM + row;
+          const bool in0 = pc.m * 2 * kTileM + row < p.H, in1 = pc.m * 2 * kTileM + kTileM + row < p.H;
+          for (int c = 0; c < n; c += 16) {
+            float v0[16], v1[16];
+            tmem_load16(d + c, v0);
+            tmem_load16(d + p.acc_cols + c, v1);
+            asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
 #pragma unroll
             for (int i = 0; i < 16; ++i)
               if (c + i < n) {
-                if (in0) yp[(size_t)(c + i) * p.H] = g[i];
-                if (in1) yp[(size_t)(c + i) * p.H + kTileM] = u[i];
+                if (in0) yp[(size_t)(c + i) * p.H] = v0[i];
+                if (in1) yp[(size_t)(c + i) * p.H + kTileM] = v1[i];
               }
-          } else if (whole) {
+          }
+        } else {
+          // A cut tile is summed by the CTA that finds the other parts written: mostly at once, as
+          // a tile's later part is the first work of the next CTA; else its own part is written
+          // too, and whoever counts the last step sums.
+          finish = whole || last_shared;
+          if (!finish) {
+            float* part = p.partial + (size_t)(cta * 2 + (pc.k0 > 0 ? 0 : 1)) * p.acc_cols * 256 + row;
+            for (int c = 0; c < n; c += 16) {
+              float g[16], u[16];
+              tmem_load16(d + c, g);
+              tmem_load16(d + p.acc_cols + c, u);
+              asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
 #pragma unroll
-            for (int i = 0; i < 16; ++i)
-              if (c + i < n && f < p.F) store_h(p, o + c + i, f, g[i], u[i]);
-          } else {
+              for (int i = 0; i < 16; ++i)
+                if (c + i < n) {
+                  __stcg(part + (c + i) * 256, g[i]);
+                  __stcg(part + (c + i) * 256 + kTileM, u[i]);
+                }
+            }
+            __threadfence();
+            epilogue_sync();
+            if (etid == 0) {
+              const unsigned mine = pc.k1 - pc.k0;
+              last_shared = atomicAdd(p.tile_steps + pc.tile, mine) + mine == (unsigned)runs.steps;
+              __threadfence();
+            }
+            epilogue_sync();
+            finish = last_shared;
+          }
+          if (finish) {
+            const int c1 = runs.cta_of(first_unit + runs.steps - 1), f = pc.m * kTileM + row;
+            if (!whole && etid == 0) p.tile_steps[pc.tile] = 0;   // ready for the next call
+            for (int c = 0; c < n; c += 16) {
+              float g[16], u[16], sg[16], su[16];
+              tmem_load16(d + c, g);
+              tmem_load16(d + p.acc_cols + c, u);
+              asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
 #pragma unroll
-            for (int i = 0; i < 16; ++i)
-              if (c + i < n) {
-                __stcg(part + (c + i) * 256, g[i]);
-                __stcg(part + (c + i) * 256 + kTileM, u[i]);
+              for (int i = 0; i < 16; ++i) sg[i] = su[i] = 0.0f;
+              for (int who = c0; who <= c1; ++who) {   // in the order of the CTAs
+                if (who != cta) {
+                  const float* from = p.partial + ((size_t)(who * 2 + (runs.start(who) > first_unit ? 0 : 1)) *
+                                                       p.acc_cols + c) * 256 + row;
+                  float vg[16], vu[16];
+#pragma unroll
+                  for (int i = 0; i < 16; ++i) {
+                    vg[i] = c + i < n ? __ldcg(from + i * 256) : 0.0f;
+                    vu[i] = c + i < n ? __ldcg(from + i * 256 + kTileM) : 0.0f;
+                  }
+#pragma unroll
+                  for (int i = 0; i < 16; ++i) { sg[i] += vg[i]; su[i] += vu[i]; }
+                } else {
+#pragma unroll
+                  for (int i = 0; i < 16; ++i) { sg[i] += g[i]; su[i] += u[i]; }
+                }
               }
+#pragma unroll
+              for (int i = 0; i < 16; ++i)
+                if (c + i < n && f < p.F) store_h(p, o + c + i, f, sg[i], su[i]);
+            }
           }
         }
         asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
         mbar_arrive(acc_empty + 8 * buf);
         buf ^= 1;
         if (buf == 0) accph ^= 1;
-        if (phase) continue;
-        if (!whole) {   // the last CTA of the tile sums the parts, in the order of the CTAs
-          __threadfence();
-          epilogue_sync();
-          if (etid == 0) {
-            const unsigned mine = pc.k1 - pc.k0;
-            const unsigned before = atomicAdd(p.tile_steps + pc.tile, mine);
-            last_shared = before + mine == (unsigned)runs.steps;
-            if (last_shared) p.tile_steps[pc.tile] = 0;   // ready for the next call
-            __threadfence();
-          }
-          epilogue_sync();
-          if (!last_shared) continue;
-          const int first_unit = pc.tile * runs.steps, c1 = runs.cta_of(first_unit + runs.steps - 1);
-          for (int i = 0; i < n; ++i) {
-            float g = 0.0f, u = 0.0f;
-            for (int c = c0; c <= c1; ++c) {
-              const float* from = p.partial + (size_t)(c * 2 + (runs.start(c) > first_unit ? 0 : 1)) * p.acc_cols * 256 +
-                                  i * 256 + row;
-              g += __ldcg(from);
-              u += __ldcg(from + kTileM);
-            }
-            if (f < p.F) store_h(p, o + i, f, g, u);
-          }
-        }
+        if (!finish) continue;
         // h is read by the copy unit of other CTAs
         asm volatile("fence.proxy.async.global;" ::: "memory");
         __threadfence();
@@ -609,32 +636,62 @@ experts_kernel(const __grid_constant__ Maps maps, const __grid_constant__ LayerP
   }
   __syncthreads();
   {
-    const int quads = p.H >> 2, items = p.tokens * quads;
-    for (int it = cta * kThreads + tid; it < items; it += gridDim.x * kThreads) {
-      const int t = it / quads, h0 = (it - t * quads) * 4;
-      float4 sum = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-      for (int j = 0; j < p.k; ++j) {
-        const int a = t * p.k + j;
-        if (pos[a] == 0xffff) continue;
+    // One warp for 128 outputs of a token (they lie in one tile of rows): lane j works out where the
+    // parts of id j are, then all lanes read four outputs of every part, eight parts at a time.
+    const int segs = (p.H + 127) >> 7, items = p.tokens * segs;
+    const size_t plane = (size_t)n_rows * p.H;
+    for (int it = cta * (kThreads / 32) + warp; it < items; it += gridDim.x * (kThreads / 32)) {
+      const int t = it / segs, h0 = (it - t * segs) * 128 + lane * 4, a = t * p.k + lane;
+      int parts = 0;
+      size_t from = 0;
+      float w = 0.0f;
+      if (lane < p.k && pos[a] != 0xffff) {
         const int u0 = (aslot[a] * runs2.per_slot + h0 / (2 * kTileM)) * runs2.steps;
-        const int planes = runs2.cta_of(u0 + runs2.steps - 1) - runs2.cta_of(u0) + 1;
-        float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-        for (int s = 0; s < planes; ++s) {
-          const float4 q = __ldcg(reinterpret_cast<const float4*>(p.yp + ((size_t)s * n_rows + pos[a]) * p.H + h0));
-          v.x += q.x; v.y += q.y; v.z += q.z; v.w += q.w;
-        }
-        const float w = p.weights[a];
-        sum.x += w * v.x; sum.y += w * v.y; sum.z += w * v.z; sum.w += w * v.w;
+        parts = runs2.cta_of(u0 + runs2.steps - 1) - runs2.cta_of(u0) + 1;
+        from = (size_t)pos[a] * p.H;
+        w = p.weights[a];
       }
-      __nv_bfloat16* y = p.y + t * p.y_stride + h0;
-      const __nv_bfloat162 lo = __floats2bfloat162_rn(sum.x, sum.y), hi = __floats2bfloat162_rn(sum.z, sum.w);
-      if ((reinterpret_cast<uintptr_t>(y) & 7) == 0) {
-        uint2 v;
-        v.x = *reinterpret_cast<const uint32_t*>(&lo);
-        v.y = *reinterpret_cast<const uint32_t*>(&hi);
-        *reinterpret_cast<uint2*>(y) = v;
-      } else {
-        y[0] = lo.x; y[1] = lo.y; y[2] = hi.x; y[3] = hi.y;
+      int upto = parts;   // parts of the ids up to and including this lane's
+#pragma unroll
+      for (int o = 1; o < 16; o <<= 1) {
+        const int v = __shfl_up_sync(0xffffffffu, upto, o);
+        if (lane >= o) upto += v;
+      }
+      const int total = __shfl_sync(0xffffffffu, upto, 15);
+      float4 sum = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+      for (int base = 0; base < total; base += 8) {
+        float4 v[8];
+        float vw[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const int c = base + i;
+          // the id that part c belongs to: the first lane whose running count exceeds it
+          const unsigned above = __ballot_sync(0xffffffffu, upto > c) & 0xffffu;
+          const int j = above ? __ffs(above) - 1 : 0;
+          const int s = c - (__shfl_sync(0xffffffffu, upto, j) - __shfl_sync(0xffffffffu, parts, j));
+          const size_t at = __shfl_sync(0xffffffffu, from, j) + s * plane;
+          vw[i] = __shfl_sync(0xffffffffu, w, j);
+          v[i] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+          if (c < total && h0 < p.H) v[i] = __ldcg(reinterpret_cast<const float4*>(p.yp + at + h0));
+          if (c >= total) vw[i] = 0.0f;
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          sum.x += vw[i] * v[i].x; sum.y += vw[i] * v[i].y;
+          sum.z += vw[i] * v[i].z; sum.w += vw[i] * v[i].w;
+        }
+      }
+      if (h0 < p.H) {
+        __nv_bfloat16* y = p.y + t * p.y_stride + h0;
+        const __nv_bfloat162 lo = __floats2bfloat162_rn(sum.x, sum.y), hi = __floats2bfloat162_rn(sum.z, sum.w);
+        if ((reinterpret_cast<uintptr_t>(y) & 7) == 0) {
+          uint2 v;
+          v.x = *reinterpret_cast<const uint32_t*>(&lo);
+          v.y = *reinterpret_cast<const uint32_t*>(&hi);
+          *reinterpret_cast<uint2*>(y) = v;
+        } else {
+          y[0] = lo.x; y[1] = lo.y; y[2] = hi.x; y[3] = hi.y;
+        }
       }
     }
   }

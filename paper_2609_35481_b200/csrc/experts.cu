@@ -16,10 +16,10 @@
 //      into the same accumulator; partial results per row go to the scratch in 32 bits.
 //   3. Every token's rows are weighted and summed, in the order of its ids.
 //
-// The work of 1 and of 2 is a list of (slot, tile of rows, step of 64 along the sum) units, cut into
-// one equal run of units for each CTA, so that all SMs stream the same number of bytes whatever
-// the sizes.  A tile cut between CTAs is summed from partial accumulators in the order of the CTAs:
-// in 1 by the CTA that finishes last (it needs the whole sum before the activation), in 2 by step 3.
+// The work of 1 and of 2 is a list of tiles of rows, each a sum over steps of 64 elements, dealt out
+// so that all SMs stream nearly the same number of bytes whatever the sizes (Schedule).  A tile cut
+// between CTAs is summed from partial accumulators in a fixed order: in 1 by the CTA that finishes
+// last (the activation needs the whole sum), in 2 by step 3.
 // Between 1 and 2 only the copies of h wait: the copies of the weights, issued by another warp, run
 // ahead and keep the memory busy while the last tiles of 1 are finished.
 //
@@ -116,8 +116,9 @@ constexpr int kMaxStages = 8;
 constexpr unsigned kWaitLimit = 1u << 25;   // polls of a wait (about a second) before it is given up
 constexpr unsigned kSpinLimit = 1u << 22;   // polls of a word in global memory (a few seconds)
 
-// Words of the workspace's control block (zero between calls).
-enum { C_STATUS = 0, C_TILES = 16, C_ARRIVE = 32, C_LEAVE = 48, C_WORDS = 64 };
+// Words of the workspace's control block.  The counters are zero between calls; the serial number
+// counts the calls and tags their parts of cut tiles.
+enum { C_STATUS = 0, C_TILES = 16, C_ARRIVE = 32, C_LEAVE = 48, C_SERIAL = 56 };
 
 struct __align__(64) Maps {
   CUtensorMap main_gu, main_down, replica_gu, replica_down, x, h;
@@ -128,8 +129,7 @@ struct LayerParams {
   const float* weights;
   __nv_bfloat16* y;
   uint32_t* control;
-  unsigned* tile_steps;      // [slots * tiles of phase 1] steps of a cut tile already summed
-  float* partial;            // [CTA][2][column][256]
+  ulonglong2* partial;       // [CTA][column][128]: parts of cut tiles
   __nv_bfloat16* h;          // [2][rows][F]: rounded value, rounded rest
   float* yp;                 // [plane][row][H]
   long long y_stride;
@@ -201,6 +201,14 @@ __device__ __forceinline__ void tmem_load16(uint32_t addr, float (&v)[16]) {
 #pragma unroll
   for (int i = 0; i < 16; ++i) v[i] = __uint_as_float(r[i]);
 }
+__device__ __forceinline__ void tmem_load8(uint32_t addr, float (&v)[8]) {
+  uint32_t r[8];
+  asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7])
+               : "r"(addr));
+#pragma unroll
+  for (int i = 0; i < 8; ++i) v[i] = __uint_as_float(r[i]);
+}
 __device__ __forceinline__ unsigned load_acquire(const unsigned* p) {
   unsigned v;
   asm volatile("ld.acquire.gpu.global.u32 %0, [%1];" : "=r"(v) : "l"(p) : "memory");
@@ -216,49 +224,78 @@ __device__ __forceinline__ bool spin_until(const unsigned* p, unsigned want) {
 }
 __device__ __forceinline__ void epilogue_sync() { asm volatile("bar.sync 1, 128;" ::: "memory"); }
 
-// The units of a phase and their division into one run a CTA.
-struct Runs {
-  int tiles, steps, per_slot, q, r;
-  __device__ Runs(int slots, int per_slot_, int steps_) {
-    per_slot = per_slot_;
-    steps = steps_;
-    tiles = slots * per_slot_;
-    const int units = tiles * steps;
-    q = units / (int)gridDim.x;
-    r = units - q * (int)gridDim.x;
-  }
+// `units` cut into `n` runs of equal length (the first ones one longer).
+struct Cut {
+  int q, r;
+  __device__ Cut(int units, int n) : q(units / n), r(units - units / n * n) {}
   __device__ int start(int c) const { return c * q + min(c, r); }
-  __device__ int cta_of(int u) const { return u < r * (q + 1) ? u / (q + 1) : r + (u - r * (q + 1)) / q; }
+  __device__ int owner(int u) const { return u < r * (q + 1) ? u / (q + 1) : r + (u - r * (q + 1)) / q; }
 };
 
 // One stretch of a tile that a CTA works on.
 struct Piece {
-  int tile, slot, m, k0, k1;
+  int tile, k0, k1;
+};
+
+// Which pieces a CTA works on, in which order.  Of `tiles` tiles of `steps` steps, tiles / CTAs go
+// whole to every CTA; the rest, fewer tiles than CTAs, go whole to one CTA each where that leaves
+// at most a sixteenth of the CTAs idle, else the steps of the rest in one row are cut into equal
+// runs.  Cut tiles come first and whole ones last, so that the parts of a cut tile are summed while
+// whole tiles stream.  The rule keeps 144 tiles whole on 148 CTAs (128 rows on nine 7168 x 2048
+// experts: phase 1 ended at 99 us, cut at 118 us) and cuts 128 (one token on eight of them: 81 us,
+// whole it would take 148 / 128 of the streaming time).
+struct Schedule {
+  int steps, tiles, n, rest, rounds;
+  bool cut_rest;
+  Cut cut;
+  __device__ Schedule(int tiles_, int steps_, int n_, bool cut_all)
+      : steps(steps_), tiles(tiles_), n(n_), cut(0, 1) {
+    rounds = cut_all ? 0 : tiles / n;
+    rest = tiles - rounds * n;
+    cut_rest = cut_all || 16 * rest < 15 * n;
+    if (cut_rest) cut = Cut(rest * steps, n);
+  }
+  // first CTA that works on a cut tile, and how many do
+  __device__ int first_cta(int tile) const { return cut.owner(tile * steps); }
+  __device__ int parts(int tile) const { return cut.owner(tile * steps + steps - 1) - first_cta(tile) + 1; }
 };
 
 struct PieceWalk {
-  const Runs& runs;
-  int u, end;
-  __device__ PieceWalk(const Runs& r, int cta) : runs(r), u(r.start(cta)), end(r.start(cta + 1)) {}
+  const Schedule& s;
+  int cta, u, end, round;
+  __device__ PieceWalk(const Schedule& sched, int cta_) : s(sched), cta(cta_), u(0), end(0), round(0) {
+    if (s.cut_rest) { u = s.cut.start(cta); end = s.cut.start(cta + 1); }
+    else if (cta < s.rest) end = 1;
+  }
   __device__ bool next(Piece& p) {
-    if (u >= end) return false;
-    p.tile = u / runs.steps;
-    p.k0 = u - p.tile * runs.steps;
-    p.k1 = min(runs.steps, p.k0 + end - u);
-    p.slot = p.tile / runs.per_slot;
-    p.m = p.tile - p.slot * runs.per_slot;
-    u += p.k1 - p.k0;
+    if (u < end) {
+      p.tile = s.cut_rest ? u / s.steps : cta;
+      p.k0 = s.cut_rest ? u - p.tile * s.steps : 0;
+      p.k1 = s.cut_rest ? min(s.steps, p.k0 + end - u) : s.steps;
+      u += p.k1 - p.k0;
+      return true;
+    }
+    if (round >= s.rounds) return false;
+    p.tile = s.rest + round * s.n + cta;
+    p.k0 = 0;
+    p.k1 = s.steps;
+    ++round;
     return true;
   }
 };
 
-struct Tables {
-  const uint16_t* act;   // [slots] instance
-  const uint16_t* off;   // [slots + 1] first row
-  const uint8_t* tok;    // [rows] token
-  const uint16_t* pos;   // [tokens * k] row of an assignment, 0xffff: ignored
-  const uint16_t* slot;  // [tokens * k] its slot
-};
+// A part of a cut tile: each 32-bit sum next to the call's tag in one 64-bit word, so that the
+// reader needs no flag and no fence, only the word.
+__device__ __forceinline__ void put_part(ulonglong2* at, float g, float u, uint32_t tag) {
+  const unsigned long long hi = (unsigned long long)tag << 32;
+  asm volatile("st.volatile.global.v2.u64 [%0], {%1, %2};" ::"l"(at), "l"(hi | __float_as_uint(g)),
+               "l"(hi | __float_as_uint(u)) : "memory");
+}
+__device__ __forceinline__ ulonglong2 get_part(const ulonglong2* at) {
+  ulonglong2 v;
+  asm volatile("ld.volatile.global.v2.u64 {%0, %1}, [%2];" : "=l"(v.x), "=l"(v.y) : "l"(at) : "memory");
+  return v;
+}
 
 __device__ __forceinline__ void store_h(const LayerParams& p, int row, int f, float g, float u) {
   const float h = g / (1.0f + expf(-g)) * u;
@@ -275,7 +312,7 @@ experts_kernel(const __grid_constant__ Maps maps, const __grid_constant__ LayerP
   __shared__ __align__(8) unsigned long long bars[2 * kMaxStages + 4];
   __shared__ uint32_t tmem_base_shared;
   __shared__ int warp_tot[3][kThreads / 32];
-  __shared__ int last_shared, failed_shared, stopped_shared;
+  __shared__ int failed_shared, stopped_shared;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, cta = blockIdx.x;
   const int A = p.tokens * p.k, N = p.instances;
   if (smem_u32(smem) & 1023) {   // the swizzled operands need it; the same in every CTA
@@ -385,8 +422,10 @@ experts_kernel(const __grid_constant__ Maps maps, const __grid_constant__ LayerP
   const uint32_t ring = smem_u32(smem), full = smem_u32(&bars[0]), empty = smem_u32(&bars[kMaxStages]);
   const uint32_t acc_full = smem_u32(&bars[2 * kMaxStages]), acc_empty = acc_full + 16;
   const int per_rank = p.e_loc + p.slots;
-  const Runs runs1(n_slots, (p.F + kTileM - 1) / kTileM, (p.H + kStepK - 1) / kStepK);
-  const Runs runs2(n_slots, (p.H + 2 * kTileM - 1) / (2 * kTileM), (p.F + kStepK - 1) / kStepK);
+  const int per_slot1 = (p.F + kTileM - 1) / kTileM, per_slot2 = (p.H + 2 * kTileM - 1) / (2 * kTileM);
+  const Schedule sched1(n_slots * per_slot1, (p.H + kStepK - 1) / kStepK, gridDim.x, false);
+  const Schedule sched2(n_slots * per_slot2, (p.F + kStepK - 1) / kStepK, gridDim.x, true);
+  const uint32_t tag = p.control[C_SERIAL] + 1;   // changed by the last CTA to leave
   volatile int *failed = &failed_shared, *stopped = &stopped_shared;
 
   if (warp == 0) {
@@ -395,16 +434,17 @@ experts_kernel(const __grid_constant__ Maps maps, const __grid_constant__ LayerP
       uint32_t ph = 0;
       bool ok = true;
       for (int phase = 0; phase < 2 && ok; ++phase) {
-        const Runs& runs = phase ? runs2 : runs1;
-        PieceWalk walk(runs, cta);
+        const Schedule& sched = phase ? sched2 : sched1;
+        const int per_slot = phase ? per_slot2 : per_slot1;
+        PieceWalk walk(sched, cta);
         Piece pc;
         while (ok && walk.next(pc)) {
-          const int inst = act[pc.slot], r = inst / per_rank, l = inst - r * per_rank;
+          const int slot = pc.tile / per_slot, m = pc.tile - slot * per_slot, inst = act[slot], r = inst / per_rank, l = inst - r * per_rank;
           const bool in_main = l < p.e_loc;
           const int z = in_main ? r * p.e_loc + l : r * p.slots + l - p.e_loc;
           const CUtensorMap* map = phase ? (in_main ? &maps.main_down : &maps.replica_down)
                                          : (in_main ? &maps.main_gu : &maps.replica_gu);
-          const int y0 = phase ? pc.m * 2 * kTileM : pc.m * kTileM;
+          const int y0 = phase ? m * 2 * kTileM : m * kTileM;
           const int y1 = phase ? y0 + kTileM : p.F + y0;
           for (int s = pc.k0; s < pc.k1; ++s) {
             if (!mbar_wait(empty + 8 * st, ph ^ 1)) { ok = false; break; }
@@ -424,14 +464,15 @@ experts_kernel(const __grid_constant__ Maps maps, const __grid_constant__ LayerP
     uint32_t ph = 0;
     bool ok = true;
     for (int phase = 0; phase < 2 && ok; ++phase) {
-      const Runs& runs = phase ? runs2 : runs1;
-      PieceWalk walk(runs, cta);
+      const Schedule& sched = phase ? sched2 : sched1;
+      const int per_slot = phase ? per_slot2 : per_slot1;
+      PieceWalk walk(sched, cta);
       Piece pc;
       bool waited = phase == 0;
       while (ok && walk.next(pc)) {
         if (!waited) {   // every tile of h is written
           int good = 1;
-          if (lane == 0) good = spin_until(p.control + C_TILES, (unsigned)runs1.tiles);
+          if (lane == 0) good = spin_until(p.control + C_TILES, (unsigned)sched1.tiles);
           ok = __shfl_sync(0xffffffffu, good, 0) != 0;
           if (!ok) break;
           __syncwarp();
@@ -441,7 +482,7 @@ experts_kernel(const __grid_constant__ Maps maps, const __grid_constant__ LayerP
         // x: four gathered rows a lane; h: 16 adjacent rows a lane, the first lanes the rounded
         // values and the next ones the rests.  Rows past the instance's last are some other row's:
         // columns of the product that nobody reads.
-        const int o = off[pc.slot], n = off[pc.slot + 1] - o;
+        const int slot = pc.tile / per_slot, o = off[slot], n = off[slot + 1] - o;
         const int groups = phase ? (n + 15) >> 4 : (n + 3) >> 2;
         const int copies = phase ? 2 * groups : groups, bytes = phase ? 2 * groups * 2048 : groups * 512;
         int row[4];
@@ -475,11 +516,12 @@ experts_kernel(const __grid_constant__ Maps maps, const __grid_constant__ LayerP
       uint32_t ph = 0, accph = 0;
       bool ok = true;
       for (int phase = 0; phase < 2 && ok; ++phase) {
-        const Runs& runs = phase ? runs2 : runs1;
-        PieceWalk walk(runs, cta);
+        const Schedule& sched = phase ? sched2 : sched1;
+        const int per_slot = phase ? per_slot2 : per_slot1;
+        PieceWalk walk(sched, cta);
         Piece pc;
         while (ok && walk.next(pc)) {
-          const int n = off[pc.slot + 1] - off[pc.slot], cols = (n + 15) & ~15;
+          const int slot = pc.tile / per_slot, n = off[slot + 1] - off[slot], cols = (n + 15) & ~15;
           const uint32_t idesc = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(cols >> 3) << 17) |
                                  ((uint32_t)(kTileM >> 4) << 24);
           if (!mbar_wait(acc_empty + 8 * buf, accph ^ 1)) { ok = false; break; }
@@ -517,27 +559,26 @@ experts_kernel(const __grid_constant__ Maps maps, const __grid_constant__ LayerP
     const int quad = warp & 3, row = quad * 32 + lane, etid = tid - 128;
     int buf = 0;
     uint32_t accph = 0;
-    bool ok = true;
-    for (int phase = 0; phase < 2 && ok; ++phase) {
-      const Runs& runs = phase ? runs2 : runs1;
-      PieceWalk walk(runs, cta);
+    bool quit = false, lost = false;   // quit is the same in all four warps, lost is a thread's own
+    for (int phase = 0; phase < 2 && !quit; ++phase) {
+      const Schedule& sched = phase ? sched2 : sched1;
+      const int per_slot = phase ? per_slot2 : per_slot1;
+      PieceWalk walk(sched, cta);
       Piece pc;
       while (walk.next(pc)) {
         if (!mbar_wait(acc_full + 8 * buf, accph)) *stopped = 1;
-        const int first_unit = pc.tile * runs.steps;
-        const bool whole = pc.k0 == 0 && pc.k1 == runs.steps;
-        if (phase == 0 && !whole && etid == 0)   // the other parts of the tile may be there already
-          last_shared = load_acquire(p.tile_steps + pc.tile) == (unsigned)(runs.steps - pc.k1 + pc.k0);
+        const int slot = pc.tile / per_slot, m = pc.tile - slot * per_slot;
+        const bool whole = pc.k0 == 0 && pc.k1 == sched.steps;
         epilogue_sync();   // the four warps go on, or stop, together
-        if (*stopped) { ok = false; break; }
+        quit = *stopped != 0;
+        if (quit) break;
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-        const int o = off[pc.slot], n = off[pc.slot + 1] - o;
-        const int c0 = runs.cta_of(first_unit);
+        const int o = off[slot], n = off[slot + 1] - o;
         const uint32_t d = tmem + buf * 2 * p.acc_cols + ((uint32_t)quad << 21);
         bool finish = false;
         if (phase) {
-          float* yp = p.yp + ((size_t)(cta - c0) * n_rows + o) * p.H + pc.m * 2 * kTileM + row;
-          const bool in0 = pc.m * 2 * kTileM + row < p.H, in1 = pc.m * 2 * kTileM + kTileM + row < p.H;
+          float* yp = p.yp + ((size_t)(cta - sched.first_cta(pc.tile)) * n_rows + o) * p.H + m * 2 * kTileM + row;
+          const bool in0 = m * 2 * kTileM + row < p.H, in1 = m * 2 * kTileM + kTileM + row < p.H;
           for (int c = 0; c < n; c += 16) {
             float v0[16], v1[16];
             tmem_load16(d + c, v0);
@@ -551,64 +592,48 @@ experts_kernel(const __grid_constant__ Maps maps, const __grid_constant__ LayerP
               }
           }
         } else {
-          // A cut tile is summed by the CTA that finds the other parts written: mostly at once, as
-          // a tile's later part is the first work of the next CTA; else its own part is written
-          // too, and whoever counts the last step sums.
-          finish = whole || last_shared;
-          if (!finish) {
-            float* part = p.partial + (size_t)(cta * 2 + (pc.k0 > 0 ? 0 : 1)) * p.acc_cols * 256 + row;
-            for (int c = 0; c < n; c += 16) {
-              float g[16], u[16];
-              tmem_load16(d + c, g);
-              tmem_load16(d + p.acc_cols + c, u);
-              asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+          // A cut tile is summed by the CTA that has its first step; the CTAs after it hold the other
+          // parts, as the first piece of theirs (so a CTA writes one part at most and nobody waits
+          // for a CTA that waits).
+          finish = pc.k0 == 0;
+          const int f = m * kTileM + row, parts = finish && !whole ? sched.parts(pc.tile) : 1;
+          for (int c = 0; c < n; c += 8) {
+            float g[8], u[8];
+            tmem_load8(d + c, g);
+            tmem_load8(d + p.acc_cols + c, u);
+            asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+            for (int part = 1; part < parts && !lost; ++part) {   // in the order of the CTAs
+              const ulonglong2* from = p.partial + ((size_t)(cta + part) * p.acc_cols + c) * kTileM + row;
+              ulonglong2 v[8];
+              bool got = false;
+              for (unsigned i = 0; i < kSpinLimit && !got; ++i) {
+                got = true;
 #pragma unroll
-              for (int i = 0; i < 16; ++i)
-                if (c + i < n) {
-                  __stcg(part + (c + i) * 256, g[i]);
-                  __stcg(part + (c + i) * 256 + kTileM, u[i]);
-                }
-            }
-            __threadfence();
-            epilogue_sync();
-            if (etid == 0) {
-              const unsigned mine = pc.k1 - pc.k0;
-              last_shared = atomicAdd(p.tile_steps + pc.tile, mine) + mine == (unsigned)runs.steps;
-              __threadfence();
-            }
-            epilogue_sync();
-            finish = last_shared;
-          }
-          if (finish) {
-            const int c1 = runs.cta_of(first_unit + runs.steps - 1), f = pc.m * kTileM + row;
-            if (!whole && etid == 0) p.tile_steps[pc.tile] = 0;   // ready for the next call
-            for (int c = 0; c < n; c += 16) {
-              float g[16], u[16], sg[16], su[16];
-              tmem_load16(d + c, g);
-              tmem_load16(d + p.acc_cols + c, u);
-              asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+                for (int j = 0; j < 8; ++j)
+                  if (c + j < n) v[j] = get_part(from + j * kTileM);
 #pragma unroll
-              for (int i = 0; i < 16; ++i) sg[i] = su[i] = 0.0f;
-              for (int who = c0; who <= c1; ++who) {   // in the order of the CTAs
-                if (who != cta) {
-                  const float* from = p.partial + ((size_t)(who * 2 + (runs.start(who) > first_unit ? 0 : 1)) *
-                                                       p.acc_cols + c) * 256 + row;
-                  float vg[16], vu[16];
-#pragma unroll
-                  for (int i = 0; i < 16; ++i) {
-                    vg[i] = c + i < n ? __ldcg(from + i * 256) : 0.0f;
-                    vu[i] = c + i < n ? __ldcg(from + i * 256 + kTileM) : 0.0f;
-                  }
-#pragma unroll
-                  for (int i = 0; i < 16; ++i) { sg[i] += vg[i]; su[i] += vu[i]; }
-                } else {
-#pragma unroll
-                  for (int i = 0; i < 16; ++i) { sg[i] += g[i]; su[i] += u[i]; }
-                }
+                for (int j = 0; j < 8; ++j)
+                  if (c + j < n) got = got && (uint32_t)(v[j].x >> 32) == tag && (uint32_t)(v[j].y >> 32) == tag;
               }
+              lost = !got;
 #pragma unroll
-              for (int i = 0; i < 16; ++i)
-                if (c + i < n && f < p.F) store_h(p, o + c + i, f, sg[i], su[i]);
+              for (int j = 0; j < 8; ++j)
+                if (c + j < n) {
+                  g[j] += __uint_as_float((uint32_t)v[j].x);
+                  u[j] += __uint_as_float((uint32_t)v[j].y);
+                }
+            }
+            if (lost) *stopped = 1;
+            __syncwarp();
+            if (!finish) {
+              ulonglong2* to = p.partial + ((size_t)cta * p.acc_cols + c) * kTileM + row;
+#pragma unroll
+              for (int j = 0; j < 8; ++j)
+                if (c + j < n) put_part(to + j * kTileM, g[j], u[j], tag);
+            } else {
+#pragma unroll
+              for (int j = 0; j < 8; ++j)
+                if (c + j < n && f < p.F) store_h(p, o + c + j, f, g[j], u[j]);
             }
           }
         }
@@ -624,7 +649,7 @@ experts_kernel(const __grid_constant__ Maps maps, const __grid_constant__ LayerP
         if (etid == 0) add_release(p.control + C_TILES, 1);
       }
     }
-    if (!ok) *failed = 1;
+    if (quit || lost) *failed = 1;
   }
 
   // ---- all partial results are written: weigh and sum
@@ -646,8 +671,7 @@ experts_kernel(const __grid_constant__ Maps maps, const __grid_constant__ LayerP
       size_t from = 0;
       float w = 0.0f;
       if (lane < p.k && pos[a] != 0xffff) {
-        const int u0 = (aslot[a] * runs2.per_slot + h0 / (2 * kTileM)) * runs2.steps;
-        parts = runs2.cta_of(u0 + runs2.steps - 1) - runs2.cta_of(u0) + 1;
+        parts = sched2.parts(aslot[a] * per_slot2 + h0 / (2 * kTileM));
         from = (size_t)pos[a] * p.H;
         w = p.weights[a];
       }
@@ -709,6 +733,7 @@ experts_kernel(const __grid_constant__ Maps maps, const __grid_constant__ LayerP
       p.control[C_TILES] = 0;
       p.control[C_ARRIVE] = 0;
       p.control[C_LEAVE] = 0;
+      p.control[C_SERIAL] += 1;
     }
   }
   if (warp == 2) {
@@ -781,7 +806,7 @@ struct topoep_experts_ctx {
   const void* replica;
   bool have_params, tiled;   // tiled: sizes that the copy unit can address
   unsigned char* ws;
-  size_t ws_bytes, off_h, off_steps, off_partial, off_yp;
+  size_t ws_bytes, off_h, off_partial, off_yp;
   EncodeFn encode;
   Maps maps;
 };
@@ -810,8 +835,8 @@ extern "C" int topoep_experts_create(topoep_experts_t* out, int ranks, int exper
   h->tiled = hidden % 8 == 0 && ffn % 8 == 0;
   h->off_h = kAlign;
   // h: 32 bits an element, or two bfloat16 parts
-  h->off_steps = h->off_h + align_up((size_t)4 * h->max_rows * ffn);
-  h->off_partial = h->off_yp = h->ws_bytes = h->off_steps;
+  h->off_partial = h->off_h + align_up((size_t)4 * h->max_rows * ffn);
+  h->off_yp = h->ws_bytes = h->off_partial;
   if (h->tiled) {
     const long long steps = (ffn + kStepK - 1) / kStepK, per_slot = (hidden + 2 * kTileM - 1) / (2 * kTileM);
     const int most = std::min(h->max_rows, h->instances);
@@ -819,9 +844,8 @@ extern "C" int topoep_experts_create(topoep_experts_t* out, int ranks, int exper
     for (int n = 1; n <= most; ++n)
       rows = std::max(rows, planes_of(n * per_slot * steps, steps) *
                                 std::min<long long>(h->max_rows, (long long)n * max_tokens));
-    h->off_partial = h->off_steps + align_up((size_t)4 * most * ((ffn + kTileM - 1) / kTileM));
     const size_t cols = (max_tokens + 15) / 16 * 16;
-    h->off_yp = h->off_partial + align_up((size_t)kMaxCtas * 2 * cols * 2 * kTileM * 4);
+    h->off_yp = h->off_partial + align_up((size_t)kMaxCtas * cols * kTileM * sizeof(ulonglong2));
     h->ws_bytes = h->off_yp + align_up((size_t)4 * rows * hidden);
   }
   *out = h;
@@ -843,7 +867,7 @@ extern "C" int topoep_experts_set_workspace(topoep_experts_t h, void* dev_ptr, s
     e = cudaGetDevice(&dev);
     if (e == cudaSuccess) e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
     h->ctas = std::min(sms, kMaxCtas);
-    if (e == cudaSuccess) e = cudaMemset(ws + h->off_steps, 0, h->off_partial - h->off_steps);
+    if (e == cudaSuccess) e = cudaMemset(ws + h->off_partial, 0, h->off_yp - h->off_partial);   // no tags
     if (e == cudaSuccess)
       e = cudaFuncSetAttribute(experts_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSharedLimit);
     if (e != cudaSuccess) return TOPOEP_ERR_CUDA;
@@ -894,8 +918,7 @@ cudaError_t launch_tiled(topoep_experts_t h, const ExpertsParams& a, cudaStream_
   p.weights = a.weights;
   p.y = a.y;
   p.control = reinterpret_cast<uint32_t*>(h->ws);
-  p.tile_steps = reinterpret_cast<unsigned*>(h->ws + h->off_steps);
-  p.partial = reinterpret_cast<float*>(h->ws + h->off_partial);
+  p.partial = reinterpret_cast<ulonglong2*>(h->ws + h->off_partial);
   p.h = reinterpret_cast<__nv_bfloat16*>(h->ws + h->off_h);
   p.yp = reinterpret_cast<float*>(h->ws + h->off_yp);
   p.y_stride = a.y_stride;

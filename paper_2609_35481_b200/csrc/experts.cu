@@ -20,8 +20,8 @@
 // so that all SMs stream nearly the same number of bytes whatever the sizes (Schedule).  A tile cut
 // between CTAs is summed from partial accumulators in a fixed order: in 1 by the CTA that finishes
 // last (the activation needs the whole sum), in 2 by step 3.
-// Between 1 and 2 only the copies of h wait: the copies of the weights, issued by another warp, run
-// ahead and keep the memory busy while the last tiles of 1 are finished.
+// Between 1 and 2 only the copies of h wait, each for its instance's tiles: the copies of the
+// weights, issued by another warp, run ahead and keep the memory busy meanwhile.
 //
 // Roles of a CTA's eight warps: 0 copies weights, 1 copies token rows, 2 issues the products, 4-7
 // read the accumulators (double-buffered in tensor memory).  The launch is cooperative: every CTA
@@ -112,13 +112,14 @@ constexpr int kTileM = 128;             // rows of one product; a stage holds tw
 constexpr int kStepK = 64;              // elements of the sum in a step: one 128-byte swizzled row
 constexpr int kHalfBytes = kTileM * kStepK * 2;
 constexpr int kStageA = 2 * kHalfBytes;
+constexpr int kIdsPerThread = 128 * 16 / kThreads;   // most tokens x most ids a token
 constexpr int kMaxStages = 8;
 constexpr unsigned kWaitLimit = 1u << 25;   // polls of a wait (about a second) before it is given up
 constexpr unsigned kSpinLimit = 1u << 22;   // polls of a word in global memory (a few seconds)
 
 // Words of the workspace's control block.  The counters are zero between calls; the serial number
 // counts the calls and tags their parts of cut tiles.
-enum { C_STATUS = 0, C_TILES = 16, C_ARRIVE = 32, C_LEAVE = 48, C_SERIAL = 56 };
+enum { C_STATUS = 0, C_ARRIVE = 32, C_LEAVE = 48, C_SERIAL = 56 };
 
 struct __align__(64) Maps {
   CUtensorMap main_gu, main_down, replica_gu, replica_down, x, h;
@@ -129,13 +130,14 @@ struct LayerParams {
   const float* weights;
   __nv_bfloat16* y;
   uint32_t* control;
+  unsigned* done;            // [slots] finished tiles of phase 1
   ulonglong2* partial;       // [CTA][column][128]: parts of cut tiles
   __nv_bfloat16* h;          // [2][rows][F]: rounded value, rounded rest
   float* yp;                 // [plane][row][H]
   long long y_stride;
   int tokens, k, H, F, e_loc, slots, instances, max_rows;
   int ring_bytes, tmem_cols, acc_cols;
-  int o_act, o_off, o_tok, o_pos, o_slot;   // offsets of the tables behind the ring
+  int o_weights, o_act, o_off, o_tok, o_pos, o_slot;   // offsets of the tables behind the ring
 };
 
 __device__ __forceinline__ uint32_t smem_u32(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
@@ -328,6 +330,11 @@ experts_kernel(const __grid_constant__ Maps maps, const __grid_constant__ LayerP
   uint8_t* tok = smem + p.o_tok;
   uint16_t* pos = reinterpret_cast<uint16_t*>(smem + p.o_pos);
   uint16_t* aslot = reinterpret_cast<uint16_t*>(smem + p.o_slot);
+  float* wts = reinterpret_cast<float*>(smem + p.o_weights);
+  int ids[kIdsPerThread];
+#pragma unroll
+  for (int i = 0; i < kIdsPerThread; ++i) ids[i] = tid + i * kThreads < A ? p.ids[tid + i * kThreads] : -1;
+  for (int i = tid; i < A; i += kThreads) wts[i] = p.weights[i];
   for (int i = tid; i < N; i += kThreads) reinterpret_cast<uint4*>(mask)[i] = make_uint4(0, 0, 0, 0);
   if (tid == 0) {
     for (int s = 0; s < kMaxStages; ++s) {
@@ -348,8 +355,9 @@ experts_kernel(const __grid_constant__ Maps maps, const __grid_constant__ LayerP
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
   }
   __syncthreads();
-  for (int a = tid; a < A; a += kThreads) {
-    const int id = p.ids[a];
+#pragma unroll
+  for (int i = 0; i < kIdsPerThread; ++i) {
+    const int a = tid + i * kThreads, id = ids[i];
     if (id >= 0 && id < N) {
       const int t = a / p.k;
       atomicOr(&mask[id * 4 + (t >> 5)], 1u << (t & 31));
@@ -395,8 +403,10 @@ experts_kernel(const __grid_constant__ Maps maps, const __grid_constant__ LayerP
   }
   if (tid == 0) off[n_slots] = (uint16_t)n_rows;
   __syncthreads();
-  for (int a = tid; a < A; a += kThreads) {
-    const int id = p.ids[a];
+#pragma unroll
+  for (int i = 0; i < kIdsPerThread; ++i) {
+    const int a = tid + i * kThreads, id = ids[i];
+    if (a >= A) break;
     uint16_t row = 0xffff, sl = 0;
     if (id >= 0 && id < N) {
       const int t = a / p.k;
@@ -468,16 +478,16 @@ experts_kernel(const __grid_constant__ Maps maps, const __grid_constant__ LayerP
       const int per_slot = phase ? per_slot2 : per_slot1;
       PieceWalk walk(sched, cta);
       Piece pc;
-      bool waited = phase == 0;
+      int ready = -1;
       while (ok && walk.next(pc)) {
-        if (!waited) {   // every tile of h is written
+        if (phase && pc.tile / per_slot != ready) {   // every tile of this slot's h is written
+          ready = pc.tile / per_slot;
           int good = 1;
-          if (lane == 0) good = spin_until(p.control + C_TILES, (unsigned)sched1.tiles);
+          if (lane == 0) good = spin_until(p.done + ready, (unsigned)per_slot1);
           ok = __shfl_sync(0xffffffffu, good, 0) != 0;
           if (!ok) break;
           __syncwarp();
           asm volatile("fence.proxy.async.global;" ::: "memory");
-          waited = true;
         }
         // x: four gathered rows a lane; h: 16 adjacent rows a lane, the first lanes the rounded
         // values and the next ones the rests.  Rows past the instance's last are some other row's:
@@ -646,7 +656,7 @@ experts_kernel(const __grid_constant__ Maps maps, const __grid_constant__ LayerP
         asm volatile("fence.proxy.async.global;" ::: "memory");
         __threadfence();
         epilogue_sync();
-        if (etid == 0) add_release(p.control + C_TILES, 1);
+        if (etid == 0) add_release(p.done + slot, 1);
       }
     }
     if (quit || lost) *failed = 1;
@@ -661,19 +671,26 @@ experts_kernel(const __grid_constant__ Maps maps, const __grid_constant__ LayerP
   }
   __syncthreads();
   {
-    // One warp for 128 outputs of a token (they lie in one tile of rows): lane j works out where the
-    // parts of id j are, then all lanes read four outputs of every part, eight parts at a time.
-    const int segs = (p.H + 127) >> 7, items = p.tokens * segs;
+    // The 256 outputs of a token that a tile of rows gives are one item: lane j works out where the
+    // parts of id j are, then all lanes read eight outputs of every part, eight parts at a time.  A
+    // warp takes an item; when there are fewer items than CTAs, the warps of a CTA share one, each
+    // taking every eighth part (one token, eight ids: 4.5 us after the last partial result with a
+    // warp an item, 2 us shared).
+    constexpr int kWarps = kThreads / 32;
+    const int items = p.tokens * per_slot2;
+    const bool shared_item = items <= (int)gridDim.x;
+    float* joint = reinterpret_cast<float*>(smem);   // [warp][256], in the ring
     const size_t plane = (size_t)n_rows * p.H;
-    for (int it = cta * (kThreads / 32) + warp; it < items; it += gridDim.x * (kThreads / 32)) {
-      const int t = it / segs, h0 = (it - t * segs) * 128 + lane * 4, a = t * p.k + lane;
+    for (int it = shared_item ? cta : cta * kWarps + warp; it < items; it += shared_item ? gridDim.x : gridDim.x * kWarps) {
+      const int t = it / per_slot2, m = it - t * per_slot2, a = t * p.k + lane;
+      const int h0 = m * 2 * kTileM + lane * 4, h1 = h0 + kTileM;
       int parts = 0;
       size_t from = 0;
       float w = 0.0f;
       if (lane < p.k && pos[a] != 0xffff) {
-        parts = sched2.parts(aslot[a] * per_slot2 + h0 / (2 * kTileM));
+        parts = sched2.parts(aslot[a] * per_slot2 + m);
         from = (size_t)pos[a] * p.H;
-        w = p.weights[a];
+        w = wts[a];
       }
       int upto = parts;   // parts of the ids up to and including this lane's
 #pragma unroll
@@ -682,32 +699,55 @@ experts_kernel(const __grid_constant__ Maps maps, const __grid_constant__ LayerP
         if (lane >= o) upto += v;
       }
       const int total = __shfl_sync(0xffffffffu, upto, 15);
-      float4 sum = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-      for (int base = 0; base < total; base += 8) {
-        float4 v[8];
+      const int step = shared_item ? kWarps : 1;
+      float sum[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
+      for (int base = shared_item ? warp : 0; base < total; base += 8 * step) {
+        float4 v[8], v2[8];
         float vw[8];
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-          const int c = base + i;
+          const int c = base + i * step;
           // the id that part c belongs to: the first lane whose running count exceeds it
           const unsigned above = __ballot_sync(0xffffffffu, upto > c) & 0xffffu;
           const int j = above ? __ffs(above) - 1 : 0;
           const int s = c - (__shfl_sync(0xffffffffu, upto, j) - __shfl_sync(0xffffffffu, parts, j));
           const size_t at = __shfl_sync(0xffffffffu, from, j) + s * plane;
           vw[i] = __shfl_sync(0xffffffffu, w, j);
-          v[i] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+          v[i] = v2[i] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
           if (c < total && h0 < p.H) v[i] = __ldcg(reinterpret_cast<const float4*>(p.yp + at + h0));
+          if (c < total && h1 < p.H) v2[i] = __ldcg(reinterpret_cast<const float4*>(p.yp + at + h1));
           if (c >= total) vw[i] = 0.0f;
         }
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-          sum.x += vw[i] * v[i].x; sum.y += vw[i] * v[i].y;
-          sum.z += vw[i] * v[i].z; sum.w += vw[i] * v[i].w;
+          sum[0] += vw[i] * v[i].x; sum[1] += vw[i] * v[i].y;
+          sum[2] += vw[i] * v[i].z; sum[3] += vw[i] * v[i].w;
+          sum[4] += vw[i] * v2[i].x; sum[5] += vw[i] * v2[i].y;
+          sum[6] += vw[i] * v2[i].z; sum[7] += vw[i] * v2[i].w;
         }
       }
-      if (h0 < p.H) {
-        __nv_bfloat16* y = p.y + t * p.y_stride + h0;
-        const __nv_bfloat162 lo = __floats2bfloat162_rn(sum.x, sum.y), hi = __floats2bfloat162_rn(sum.z, sum.w);
+      if (shared_item) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) joint[warp * 256 + i * 32 + lane] = sum[i];
+        __syncthreads();
+        if (warp == 0) {
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            sum[i] = 0.0f;
+#pragma unroll
+            for (int o = 0; o < kWarps; ++o) sum[i] += joint[o * 256 + i * 32 + lane];
+          }
+        }
+        __syncthreads();
+        if (warp != 0) continue;
+      }
+#pragma unroll
+      for (int half = 0; half < 2; ++half) {
+        const int hh = half ? h1 : h0;
+        if (hh >= p.H) continue;
+        __nv_bfloat16* y = p.y + t * p.y_stride + hh;
+        const __nv_bfloat162 lo = __floats2bfloat162_rn(sum[4 * half], sum[4 * half + 1]);
+        const __nv_bfloat162 hi = __floats2bfloat162_rn(sum[4 * half + 2], sum[4 * half + 3]);
         if ((reinterpret_cast<uintptr_t>(y) & 7) == 0) {
           uint2 v;
           v.x = *reinterpret_cast<const uint32_t*>(&lo);
@@ -727,10 +767,11 @@ experts_kernel(const __grid_constant__ Maps maps, const __grid_constant__ LayerP
     }
     __syncthreads();
   }
+  if (cta == 0)   // every CTA is past its waits for h
+    for (int i = tid; i < n_slots; i += kThreads) p.done[i] = 0;
   if (tid == 0) {   // the last CTA to leave makes the counters ready for the next call
     const unsigned before = atomicAdd(p.control + C_LEAVE, 1);
     if (before + 1 == gridDim.x) {
-      p.control[C_TILES] = 0;
       p.control[C_ARRIVE] = 0;
       p.control[C_LEAVE] = 0;
       p.control[C_SERIAL] += 1;
@@ -783,9 +824,9 @@ struct Shape {
   size_t bytes;
   Shape(int tokens, int k, int instances) {
     const int a = tokens * k, slots = std::min(a, instances);
-    const size_t tables = 2 * (size_t)slots + 2 * ((size_t)slots + 2) + (a + 1) / 2 * 2 + 4 * (size_t)a + 16;
+    const size_t tables = 2 * (size_t)slots + 2 * ((size_t)slots + 2) + (a + 1) / 2 * 2 + 8 * (size_t)a + 16;
     ring = (int)((kSharedLimit - tables) / 1024 * 1024);
-    o_act = ring;
+    o_act = ring + 4 * a;   // weights first
     o_off = o_act + 2 * slots;
     o_pos = o_off + 2 * (slots + 2);
     o_slot = o_pos + 2 * a;
@@ -833,7 +874,7 @@ extern "C" int topoep_experts_create(topoep_experts_t* out, int ranks, int exper
   h->max_rows = max_tokens * top_k;
   // rows of both matrices start on 16 bytes, as the copy unit needs them
   h->tiled = hidden % 8 == 0 && ffn % 8 == 0;
-  h->off_h = kAlign;
+  h->off_h = kAlign + align_up((size_t)4 * std::min(h->max_rows, h->instances));   // control, counters
   // h: 32 bits an element, or two bfloat16 parts
   h->off_partial = h->off_h + align_up((size_t)4 * h->max_rows * ffn);
   h->off_yp = h->ws_bytes = h->off_partial;
@@ -861,7 +902,7 @@ extern "C" int topoep_experts_set_workspace(topoep_experts_t h, void* dev_ptr, s
   if (bytes < h->ws_bytes || !aligned_to(dev_ptr, kAlign)) return TOPOEP_ERR_WORKSPACE;
   h->ws = nullptr;
   unsigned char* ws = static_cast<unsigned char*>(dev_ptr);
-  cudaError_t e = cudaMemset(ws, 0, kAlign);
+  cudaError_t e = cudaMemset(ws, 0, h->off_h);
   if (e == cudaSuccess && h->tiled) {
     int dev = 0, sms = 0;
     e = cudaGetDevice(&dev);
@@ -918,6 +959,7 @@ cudaError_t launch_tiled(topoep_experts_t h, const ExpertsParams& a, cudaStream_
   p.weights = a.weights;
   p.y = a.y;
   p.control = reinterpret_cast<uint32_t*>(h->ws);
+  p.done = reinterpret_cast<unsigned*>(h->ws + kAlign);
   p.partial = reinterpret_cast<ulonglong2*>(h->ws + h->off_partial);
   p.h = reinterpret_cast<__nv_bfloat16*>(h->ws + h->off_h);
   p.yp = reinterpret_cast<float*>(h->ws + h->off_yp);
@@ -934,6 +976,7 @@ cudaError_t launch_tiled(topoep_experts_t h, const ExpertsParams& a, cudaStream_
   p.acc_cols = (a.tokens + 15) / 16 * 16;
   p.tmem_cols = 32;
   while (p.tmem_cols < 4 * p.acc_cols) p.tmem_cols *= 2;
+  p.o_weights = sh.ring;
   p.o_act = sh.o_act;
   p.o_off = sh.o_off;
   p.o_tok = sh.o_tok;

@@ -1,8 +1,22 @@
 // Global norm of many gradient tensors and clipping (definition in topoep.h).
 //
-// Bound by memory: every element is read for the norm, then read again and written for the
-// scaling.  The list of tensors is cut into chunks of kChunk elements of one tensor; blocks walk
-// the chunks blockIdx.x, blockIdx.x + gridDim.x, ...
+// Bound by memory.  One cooperative kernel: all warps read the tensors once for the norm, every
+// CTA publishes its sum, every CTA adds all of them up in the same order, and the warps read their
+// chunks again, scale and write them.  N bytes of gradients cannot do with less than 3 N of traffic
+// (read, read, write) except for what the second read still finds on the chip, so
+//   * the second pass walks a warp's chunks from the last back to the first, and the first pass
+//     marks what comes before the last kKeepBytes as not worth keeping in L2;
+//   * with a factor of 1 in place nothing is read or written again.
+//
+// The list is cut into chunks of a few KB of adjacent elements when it is created, one chunk a warp
+// at a time: lanes read 16 bytes, four of them in flight, with single elements at a tensor's
+// ragged ends.  Rows shorter than a chunk, and outputs that lie otherwise than their gradients
+// relative to 16 bytes, go element by element.
+//
+// Squares are summed in 32 bits over the (at most) 64 bytes a lane holds in flight and added up in
+// 64 bits beyond that; a sum of squares outside [2^-60, 2^126] (gradients so small or large that
+// squares leave the range, zeros, infinities, NaN) is formed again in 64 bits from the same
+// registers.
 #include <climits>
 #include <cmath>
 #include <new>
@@ -15,112 +29,293 @@ namespace topoep {
 namespace {
 
 constexpr int kClipThreads = 512;
-constexpr int kChunk = 16384;           // elements of a chunk
-constexpr int kMaxBlocks = 2048;        // partial results in the workspace
+constexpr int kClipWarps = kClipThreads / 32;
+constexpr int kCtasPerSm = 2;
+constexpr int kMaxCtas = 320;            // partial results in the workspace
+constexpr int kMinChunkBytes = 2048, kMaxChunkBytes = 16384;
+constexpr int kStridedElements = 2048;   // of a chunk of short rows
+constexpr long long kKeepBytes = 64ll << 20;
+constexpr unsigned kSpinLimit = 1u << 22;   // polls of a word (a few seconds) before giving up
 constexpr float kClipEps = 1e-6f;
 
-struct ClipTensor {
+// Adjacent elements src[0 .. n) -> dst[0 .. n); with `tensor` >= 0, n elements of a tensor of short
+// rows beginning with element `first` of it.
+struct ClipChunk {
   const void* src;
   void* dst;
-  long long cols, src_stride, dst_stride, elements;
-  long long first_chunk;
-  int dtype, pad;
+  int n;
+  int dtype;
+  int tensor;
+  int scalar;   // 1: source and output differ modulo 16 bytes
+  long long first;
+};
+
+struct ClipRows {
+  long long cols, src_stride, dst_stride;
 };
 
 struct ClipParams {
-  const ClipTensor* tensors;
-  double* partial;
+  const ClipChunk* chunks;
+  const ClipRows* rows;
+  ulonglong2* partial;     // [CTA] the two halves of a sum, each with the call's tag
+  uint32_t* control;       // serial number, CTAs that left, status
   float* norm;
-  long long chunks;
-  int count, kind, blocks;
+  long long n_chunks, keep_from;
+  int kind, scale;
   float max_norm;
 };
-
-// Index of the tensor that holds chunk c: the last one whose first chunk is not above c.
-__device__ __forceinline__ int tensor_of(const ClipParams& p, long long c) {
-  int lo = 0, hi = p.count - 1;
-  while (lo < hi) {
-    const int mid = (lo + hi + 1) >> 1;
-    if (p.tensors[mid].first_chunk <= c) lo = mid; else hi = mid - 1;
-  }
-  return lo;
-}
-
-__device__ __forceinline__ long long offset_of(const ClipTensor& t, long long i, long long stride) {
-  return stride == t.cols ? i : i / t.cols * stride + i % t.cols;
-}
+enum { C_SERIAL = 0, C_LEAVE = 16, C_STATUS = 32 };
 
 __device__ __forceinline__ double join(double a, double b, int kind) {
   if (kind == 0) return a + b;
   return isnan(a) ? a : isnan(b) ? b : fmax(a, b);
 }
 
+// 16 bytes as 32-bit values.
+template <typename T> struct Vec;
+template <> struct Vec<float> {
+  static constexpr int N = 4;
+  static __device__ __forceinline__ void get(const uint4& v, float (&f)[4]) {
+    f[0] = __uint_as_float(v.x); f[1] = __uint_as_float(v.y); f[2] = __uint_as_float(v.z); f[3] = __uint_as_float(v.w);
+  }
+  static __device__ __forceinline__ uint4 put(const float (&f)[4]) {
+    return make_uint4(__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]), __float_as_uint(f[3]));
+  }
+};
+template <> struct Vec<__nv_bfloat16> {
+  static constexpr int N = 8;
+  static __device__ __forceinline__ void get(const uint4& v, float (&f)[8]) {
+    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) { f[2 * i] = __uint_as_float(w[i] << 16); f[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u); }
+  }
+  static __device__ __forceinline__ uint4 put(const float (&f)[8]) {
+    uint32_t w[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const __nv_bfloat162 h = __floats2bfloat162_rn(f[2 * i], f[2 * i + 1]);
+      w[i] = *reinterpret_cast<const uint32_t*>(&h);
+    }
+    return make_uint4(w[0], w[1], w[2], w[3]);
+  }
+};
+template <> struct Vec<__half> {
+  static constexpr int N = 8;
+  static __device__ __forceinline__ void get(const uint4& v, float (&f)[8]) {
+    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float2 p = __half22float2(*reinterpret_cast<const __half2*>(&w[i]));
+      f[2 * i] = p.x; f[2 * i + 1] = p.y;
+    }
+  }
+  static __device__ __forceinline__ uint4 put(const float (&f)[8]) {
+    uint32_t w[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const __half2 h = __floats2half2_rn(f[2 * i], f[2 * i + 1]);
+      w[i] = *reinterpret_cast<const uint32_t*>(&h);
+    }
+    return make_uint4(w[0], w[1], w[2], w[3]);
+  }
+};
+
+// What four vectors (or fewer: the rest are zero) add to the sum or maximum.
 template <typename T>
-__device__ __forceinline__ void add_chunk(const ClipTensor& t, long long first, int kind, double* sum) {
-  const T* src = static_cast<const T*>(t.src);
-  const long long last = min(first + (long long)kChunk, t.elements);
-  for (long long i = first + threadIdx.x; i < last; i += kClipThreads) {
-    const float g = to_f32(src[offset_of(t, i, t.src_stride)]);
-    if (kind == 0) *sum += (double)g * g;
-    else *sum = join(*sum, fabs((double)g), kind);
+__device__ __forceinline__ double take(const uint4 (&v)[4], int kind) {
+  constexpr int N = Vec<T>::N;
+  if (kind == 0) {
+    float s[N];
+#pragma unroll
+    for (int i = 0; i < N; ++i) s[i] = 0.0f;
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      float f[N];
+      Vec<T>::get(v[q], f);
+#pragma unroll
+      for (int i = 0; i < N; ++i) s[i] = fmaf(f[i], f[i], s[i]);
+    }
+#pragma unroll
+    for (int o = N / 2; o; o >>= 1)
+#pragma unroll
+      for (int i = 0; i < N / 2; ++i)
+        if (i < o) s[i] += s[i + o];
+    if (s[0] >= 0x1p-60f && s[0] <= 0x1p126f) return (double)s[0];
+    double d = 0.0;
+#pragma unroll 1
+    for (int q = 0; q < 4; ++q) {
+      float f[N];
+      Vec<T>::get(q == 0 ? v[0] : q == 1 ? v[1] : q == 2 ? v[2] : v[3], f);
+#pragma unroll
+      for (int i = 0; i < N; ++i) d += (double)f[i] * f[i];
+    }
+    return d;
+  }
+  double m = 0.0;
+#pragma unroll
+  for (int q = 0; q < 4; ++q) {
+    float f[N], top = 0.0f;
+    Vec<T>::get(v[q], f);
+#pragma unroll
+    for (int i = 0; i < N; ++i) top = fabsf(f[i]) <= top ? top : isnan(top) ? top : fabsf(f[i]);
+    m = join(m, top, 1);
+  }
+  return m;
+}
+
+template <typename T>
+__device__ __forceinline__ double take_one(T v, int kind) {
+  const double g = (double)to_f32(v);
+  return kind == 0 ? g * g : fabs(g);
+}
+
+__device__ __forceinline__ long long offset_of(long long i, long long cols, long long stride) {
+  return i / cols * stride + i % cols;
+}
+
+template <typename T>
+__device__ __forceinline__ double norm_chunk(const ClipParams& p, const ClipChunk& c, int kind, bool keep, int lane) {
+  double sum = 0.0;
+  const T* src = static_cast<const T*>(c.src);
+  if (c.tensor >= 0) {
+    const ClipRows r = p.rows[c.tensor];
+    for (int i = lane; i < c.n; i += 32)
+      sum = join(sum, take_one(src[offset_of(c.first + i, r.cols, r.src_stride)], kind), kind);
+    return sum;
+  }
+  const int head = min(c.n, (int)(((16 - (reinterpret_cast<uintptr_t>(src) & 15)) & 15) / sizeof(T)));
+  const int vecs = (c.n - head) / Vec<T>::N, tail = head + vecs * Vec<T>::N;
+  if (lane < head) sum = take_one(src[lane], kind);
+  if (lane < c.n - tail) sum = join(sum, take_one(src[tail + lane], kind), kind);
+  const uint4* body = reinterpret_cast<const uint4*>(src + head);
+  for (int at = lane; at < vecs; at += 128) {
+    uint4 v[4];
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      v[q] = make_uint4(0, 0, 0, 0);
+      if (at + 32 * q < vecs) v[q] = keep ? __ldcg(body + at + 32 * q) : __ldcs(body + at + 32 * q);
+    }
+    sum = join(sum, take<T>(v, kind), kind);
+  }
+  return sum;
+}
+
+template <typename T>
+__device__ __forceinline__ void scale_chunk(const ClipParams& p, const ClipChunk& c, float factor, int lane) {
+  const T* src = static_cast<const T*>(c.src);
+  T* dst = static_cast<T*>(c.dst);
+  if (c.tensor >= 0) {
+    const ClipRows r = p.rows[c.tensor];
+    for (int i = lane; i < c.n; i += 32)
+      dst[offset_of(c.first + i, r.cols, r.dst_stride)] =
+          from_f32<T>(to_f32(src[offset_of(c.first + i, r.cols, r.src_stride)]) * factor);
+    return;
+  }
+  if (c.scalar) {
+    for (int i = lane; i < c.n; i += 32) dst[i] = from_f32<T>(to_f32(src[i]) * factor);
+    return;
+  }
+  const int head = min(c.n, (int)(((16 - (reinterpret_cast<uintptr_t>(src) & 15)) & 15) / sizeof(T)));
+  const int vecs = (c.n - head) / Vec<T>::N, tail = head + vecs * Vec<T>::N;
+  if (lane < head) dst[lane] = from_f32<T>(to_f32(src[lane]) * factor);
+  if (lane < c.n - tail) dst[tail + lane] = from_f32<T>(to_f32(src[tail + lane]) * factor);
+  const uint4* body = reinterpret_cast<const uint4*>(src + head);
+  uint4* out = reinterpret_cast<uint4*>(dst + head);
+  for (int at = lane; at < vecs; at += 128) {
+    uint4 v[4];
+#pragma unroll
+    for (int q = 0; q < 4; ++q)
+      if (at + 32 * q < vecs) v[q] = __ldcs(body + at + 32 * q);
+#pragma unroll
+    for (int q = 0; q < 4; ++q)
+      if (at + 32 * q < vecs) {
+        float f[Vec<T>::N];
+        Vec<T>::get(v[q], f);
+#pragma unroll
+        for (int i = 0; i < Vec<T>::N; ++i) f[i] *= factor;
+        __stcs(out + at + 32 * q, Vec<T>::put(f));
+      }
   }
 }
 
-// Sum (or maximum) over the block in a fixed order; the result is in every thread of warp 0.
+// Sum (or maximum) over the block in a fixed order; valid in every thread.
 __device__ double block_join(double v, int kind, double* shared) {
+#pragma unroll
   for (int o = 16; o; o >>= 1) v = join(v, __shfl_xor_sync(0xffffffffu, v, o), kind);
   if ((threadIdx.x & 31) == 0) shared[threadIdx.x >> 5] = v;
   __syncthreads();
-  v = (threadIdx.x & 31) < kClipThreads / 32 ? shared[threadIdx.x & 31] : 0.0;
+  v = (threadIdx.x & 31) < kClipWarps ? shared[threadIdx.x & 31] : 0.0;
+#pragma unroll
   for (int o = 16; o; o >>= 1) v = join(v, __shfl_xor_sync(0xffffffffu, v, o), kind);
   __syncthreads();
   return v;
 }
 
-__global__ void __launch_bounds__(kClipThreads) clip_norm_kernel(const ClipParams p) {
+__global__ void __launch_bounds__(kClipThreads, kCtasPerSm) clip_kernel(const ClipParams p) {
   __shared__ double shared[32];
+  __shared__ int failed;
+  const int lane = threadIdx.x & 31, warps = gridDim.x * kClipWarps;
+  // neighbouring chunks go to different CTAs: a short list still reaches all of them
+  const int warp = (threadIdx.x >> 5) * gridDim.x + blockIdx.x;
+  const uint32_t tag = p.control[C_SERIAL] + 1;   // changed by the last CTA to leave
+  if (threadIdx.x == 0) failed = 0;
+
   double sum = 0.0;
-  for (long long c = blockIdx.x; c < p.chunks; c += gridDim.x) {
-    const ClipTensor t = p.tensors[tensor_of(p, c)];
-    const long long first = (c - t.first_chunk) * kChunk;
-    if (t.dtype == TOPOEP_DTYPE_F32) add_chunk<float>(t, first, p.kind, &sum);
-    else if (t.dtype == TOPOEP_DTYPE_BF16) add_chunk<__nv_bfloat16>(t, first, p.kind, &sum);
-    else add_chunk<__half>(t, first, p.kind, &sum);
+  for (long long i = warp; i < p.n_chunks; i += warps) {
+    const ClipChunk c = p.chunks[i];
+    const bool keep = i >= p.keep_from;
+    double v;
+    if (c.dtype == TOPOEP_DTYPE_BF16) v = norm_chunk<__nv_bfloat16>(p, c, p.kind, keep, lane);
+    else if (c.dtype == TOPOEP_DTYPE_F32) v = norm_chunk<float>(p, c, p.kind, keep, lane);
+    else v = norm_chunk<__half>(p, c, p.kind, keep, lane);
+    sum = join(sum, v, p.kind);
   }
   sum = block_join(sum, p.kind, shared);
-  if (threadIdx.x == 0) p.partial[blockIdx.x] = sum;
-}
 
-template <typename T>
-__device__ __forceinline__ void scale_chunk(const ClipTensor& t, long long first, float factor) {
-  const T* src = static_cast<const T*>(t.src);
-  T* dst = static_cast<T*>(t.dst);
-  const long long last = min(first + (long long)kChunk, t.elements);
-  for (long long i = first + threadIdx.x; i < last; i += kClipThreads)
-    dst[offset_of(t, i, t.dst_stride)] = from_f32<T>(to_f32(src[offset_of(t, i, t.src_stride)]) * factor);
-}
-
-__global__ void __launch_bounds__(kClipThreads) clip_scale_kernel(const ClipParams p, int scale) {
-  __shared__ double shared[32];
-  __shared__ float factor_shared;
-  double sum = 0.0;
-  for (int i = threadIdx.x; i < p.blocks; i += kClipThreads) sum = join(sum, p.partial[i], p.kind);
-  sum = block_join(sum, p.kind, shared);
-  if (threadIdx.x == 0) {
+  const bool reads = p.scale || blockIdx.x == 0;
+  if (gridDim.x > 1) {
+    if (threadIdx.x == 0) {
+      const unsigned long long bits = __double_as_longlong(sum), hi = (unsigned long long)tag << 32;
+      asm volatile("st.volatile.global.v2.u64 [%0], {%1, %2};" ::"l"(p.partial + blockIdx.x),
+                   "l"(hi | (bits & 0xffffffffu)), "l"(hi | (bits >> 32)) : "memory");
+    }
+    if (reads) {
+      sum = 0.0;
+      if (threadIdx.x < gridDim.x) {
+        unsigned long long a = 0, b = 0;
+        bool got = false;
+        for (unsigned i = 0; i < kSpinLimit && !got; ++i) {
+          asm volatile("ld.volatile.global.v2.u64 {%0, %1}, [%2];" : "=l"(a), "=l"(b) : "l"(p.partial + threadIdx.x) : "memory");
+          got = (uint32_t)(a >> 32) == tag && (uint32_t)(b >> 32) == tag;
+        }
+        sum = __longlong_as_double((b << 32) | (a & 0xffffffffu));
+        if (!got) { failed = 1; sum = __longlong_as_double(0x7ff8000000000000ll); }
+      }
+      sum = block_join(sum, p.kind, shared);
+    }
+  }
+  if (reads) {
     const float norm = (float)(p.kind == 0 ? sqrt(sum) : sum);
-    if (blockIdx.x == 0) *p.norm = norm;
-    const float f = p.max_norm / (norm + kClipEps);
-    factor_shared = f > 1.0f ? 1.0f : f;   // a NaN stays
+    if (blockIdx.x == 0 && threadIdx.x == 0) *p.norm = norm;
+    if (p.scale && !failed) {
+      const float f = p.max_norm / (norm + kClipEps), factor = f > 1.0f ? 1.0f : f;   // a NaN stays
+      const long long mine = warp < p.n_chunks ? (p.n_chunks - warp + warps - 1) / warps : 0;
+      for (long long k = mine; k-- > 0;) {
+        const ClipChunk c = p.chunks[warp + k * warps];
+        if (factor == 1.0f && c.dst == c.src) continue;
+        if (c.dtype == TOPOEP_DTYPE_BF16) scale_chunk<__nv_bfloat16>(p, c, factor, lane);
+        else if (c.dtype == TOPOEP_DTYPE_F32) scale_chunk<float>(p, c, factor, lane);
+        else scale_chunk<__half>(p, c, factor, lane);
+      }
+    }
   }
-  __syncthreads();
-  if (!scale) return;
-  const float factor = factor_shared;
-  for (long long c = blockIdx.x; c < p.chunks; c += gridDim.x) {
-    const ClipTensor t = p.tensors[tensor_of(p, c)];
-    const long long first = (c - t.first_chunk) * kChunk;
-    if (t.dtype == TOPOEP_DTYPE_F32) scale_chunk<float>(t, first, factor);
-    else if (t.dtype == TOPOEP_DTYPE_BF16) scale_chunk<__nv_bfloat16>(t, first, factor);
-    else scale_chunk<__half>(t, first, factor);
+  if (threadIdx.x == 0) {
+    if (failed) atomicOr(p.control + C_STATUS, TOPOEP_FLAG_INTERNAL);
+    // every CTA has read the serial number; what it published was read, or is never asked for
+    if (atomicAdd(p.control + C_LEAVE, 1) + 1 == gridDim.x) {
+      p.control[C_LEAVE] = 0;
+      p.control[C_SERIAL] = tag;
+    }
   }
 }
 
@@ -134,52 +329,105 @@ inline size_t align_up(size_t x) { return (x + kAlign - 1) / kAlign * kAlign; }
 using namespace topoep;
 
 struct topoep_clip_ctx {
-  std::vector<ClipTensor> tensors;
-  long long chunks;
+  std::vector<ClipChunk> chunks;
+  std::vector<ClipRows> rows;
+  long long keep_from;
   unsigned char* ws;
-  size_t off_tensors, ws_bytes;
-  int sms;
+  size_t off_partial, off_rows, off_chunks, ws_bytes;
+  int ctas;
 };
+
+// Appends the chunks of n adjacent elements; the first cut makes the later ones start on 16 bytes.
+static void cut_run(topoep_clip_ctx* h, const char* src, char* dst, long long n, int dtype, long long chunk_bytes) {
+  const long long size = (long long)dtype_bytes(dtype), odd = (long long)(reinterpret_cast<uintptr_t>(src) & 15);
+  long long at = 0;
+  while (at < n) {
+    const long long room = (chunk_bytes - (at == 0 ? odd : 0)) / size;
+    ClipChunk c = {};
+    c.src = src + at * size;
+    c.dst = dst + at * size;
+    c.n = (int)(n - at < room ? n - at : room);
+    c.dtype = dtype;
+    c.tensor = -1;
+    c.scalar = ((reinterpret_cast<uintptr_t>(src) ^ reinterpret_cast<uintptr_t>(dst)) & 15) != 0;
+    h->chunks.push_back(c);
+    at += c.n;
+  }
+}
+
+static int list_chunks(topoep_clip_ctx* h, int64_t count, const topoep_grad_tensor* tensors) {
+  double total = 0.0;
+  for (int64_t i = 0; i < count; ++i) {
+    const topoep_grad_tensor& g = tensors[i];
+    if (!dtype_known(g.dtype)) return TOPOEP_ERR_ARG;
+    if (g.rows < 0 || g.cols < 0 || (g.cols > 0 && g.rows > (1ll << 48) / g.cols)) return TOPOEP_ERR_SIZE;
+    if (g.rows == 0 || g.cols == 0) continue;
+    if (!g.src) return TOPOEP_ERR_NULL;
+    const int64_t dst_stride = g.dst ? g.dst_row_stride : g.src_row_stride;
+    if (g.rows > 1 && (g.src_row_stride < g.cols || g.src_row_stride > (1ll << 40) || dst_stride < g.cols ||
+                       dst_stride > (1ll << 40)))
+      return TOPOEP_ERR_SIZE;
+    if (g.rows > 1 && (!g.dst || g.dst == g.src) && g.src_row_stride != dst_stride) return TOPOEP_ERR_ARG;
+    if (!aligned_to(g.src, dtype_bytes(g.dtype)) || !aligned_to(g.dst, dtype_bytes(g.dtype))) return TOPOEP_ERR_ALIGN;
+    total += (double)g.rows * g.cols * dtype_bytes(g.dtype);
+  }
+  // a few chunks for each warp of a full grid, within the limits
+  long long chunk_bytes = kMinChunkBytes;
+  while (chunk_bytes < kMaxChunkBytes && total > 4.0 * chunk_bytes * 148 * kCtasPerSm * kClipWarps) chunk_bytes *= 2;
+  for (int64_t i = 0; i < count; ++i) {
+    const topoep_grad_tensor& g = tensors[i];
+    if (g.rows == 0 || g.cols == 0) continue;
+    const char* src = static_cast<const char*>(g.src);
+    char* dst = g.dst ? static_cast<char*>(g.dst) : const_cast<char*>(src);
+    const long long size = (long long)dtype_bytes(g.dtype);
+    const long long ss = g.rows > 1 ? g.src_row_stride : g.cols;
+    const long long ds = g.rows > 1 ? (g.dst ? g.dst_row_stride : g.src_row_stride) : g.cols;
+    if (ss == g.cols && ds == g.cols) {
+      cut_run(h, src, dst, g.rows * g.cols, g.dtype, chunk_bytes);
+    } else if (g.cols * size >= kMinChunkBytes) {
+      for (int64_t r = 0; r < g.rows; ++r) cut_run(h, src + r * ss * size, dst + r * ds * size, g.cols, g.dtype, chunk_bytes);
+    } else {
+      const ClipRows rows = {g.cols, ss, ds};
+      const long long n = g.rows * g.cols;
+      for (long long at = 0; at < n; at += kStridedElements) {
+        ClipChunk c = {};
+        c.src = src;
+        c.dst = dst;
+        c.n = (int)(n - at < kStridedElements ? n - at : kStridedElements);
+        c.dtype = g.dtype;
+        c.tensor = (int)h->rows.size();
+        c.first = at;
+        h->chunks.push_back(c);
+      }
+      h->rows.push_back(rows);
+    }
+  }
+  // the chunks of the last kKeepBytes may still be in L2 when the second pass begins with them
+  long long kept = 0;
+  h->keep_from = (long long)h->chunks.size();
+  while (h->keep_from > 0 && kept < kKeepBytes) {
+    const ClipChunk& c = h->chunks[--h->keep_from];
+    kept += c.n * (long long)dtype_bytes(c.dtype);
+  }
+  return TOPOEP_OK;
+}
 
 extern "C" int topoep_clip_create(topoep_clip_t* out, int64_t count, const topoep_grad_tensor* tensors) {
   if (!out || (count > 0 && !tensors)) return TOPOEP_ERR_NULL;
   if (count < 0 || count > (1 << 24)) return TOPOEP_ERR_SIZE;
   topoep_clip_ctx* h = new (std::nothrow) topoep_clip_ctx();
   if (!h) return TOPOEP_ERR_CONFIG;
-  int rc = TOPOEP_OK;
+  int rc;
   try {
-    h->chunks = 0;
-    for (int64_t i = 0; i < count && rc == TOPOEP_OK; ++i) {
-      const topoep_grad_tensor& g = tensors[i];
-      if (!dtype_known(g.dtype)) { rc = TOPOEP_ERR_ARG; break; }
-      if (g.rows < 0 || g.cols < 0 || (g.cols > 0 && g.rows > (1ll << 48) / g.cols)) { rc = TOPOEP_ERR_SIZE; break; }
-      if (g.rows == 0 || g.cols == 0) continue;
-      if (!g.src) { rc = TOPOEP_ERR_NULL; break; }
-      const bool in_place = !g.dst || g.dst == g.src;
-      if (g.rows > 1 && (g.src_row_stride < g.cols || g.src_row_stride > (1ll << 40))) { rc = TOPOEP_ERR_SIZE; break; }
-      const int64_t dst_stride = g.dst ? g.dst_row_stride : g.src_row_stride;
-      if (g.rows > 1 && (dst_stride < g.cols || dst_stride > (1ll << 40))) { rc = TOPOEP_ERR_SIZE; break; }
-      if (in_place && g.rows > 1 && g.src_row_stride != dst_stride) { rc = TOPOEP_ERR_ARG; break; }
-      const size_t bytes = dtype_bytes(g.dtype);
-      if (!aligned_to(g.src, bytes) || !aligned_to(g.dst, bytes)) { rc = TOPOEP_ERR_ALIGN; break; }
-      ClipTensor t = {};
-      t.src = g.src;
-      t.dst = in_place ? const_cast<void*>(g.src) : g.dst;
-      t.cols = g.cols;
-      t.src_stride = g.rows > 1 ? g.src_row_stride : g.cols;
-      t.dst_stride = g.rows > 1 ? dst_stride : g.cols;
-      t.elements = g.rows * g.cols;
-      t.first_chunk = h->chunks;
-      t.dtype = g.dtype;
-      h->chunks += (t.elements + kChunk - 1) / kChunk;
-      h->tensors.push_back(t);
-    }
-  } catch (...) {
+    rc = list_chunks(h, count, tensors);
+  } catch (...) {   // no host memory for the list
     rc = TOPOEP_ERR_CONFIG;
   }
   if (rc != TOPOEP_OK) { delete h; return rc; }
-  h->off_tensors = align_up(sizeof(double) * kMaxBlocks);
-  h->ws_bytes = h->off_tensors + align_up(sizeof(ClipTensor) * h->tensors.size());
+  h->off_partial = kAlign;
+  h->off_rows = h->off_partial + align_up(sizeof(ulonglong2) * kMaxCtas);
+  h->off_chunks = h->off_rows + align_up(sizeof(ClipRows) * h->rows.size());
+  h->ws_bytes = h->off_chunks + align_up(sizeof(ClipChunk) * h->chunks.size());
   *out = h;
   return TOPOEP_OK;
 }
@@ -193,14 +441,21 @@ extern "C" int topoep_clip_set_workspace(topoep_clip_t h, void* dev_ptr, size_t 
   if (bytes < h->ws_bytes || !aligned_to(dev_ptr, kAlign)) return TOPOEP_ERR_WORKSPACE;
   h->ws = nullptr;
   unsigned char* ws = static_cast<unsigned char*>(dev_ptr);
-  int dev = 0;
+  int dev = 0, sms = 0;
   cudaError_t e = cudaGetDevice(&dev);
-  if (e == cudaSuccess) e = cudaDeviceGetAttribute(&h->sms, cudaDevAttrMultiProcessorCount, dev);
-  if (e == cudaSuccess && !h->tensors.empty())
-    e = cudaMemcpy(ws + h->off_tensors, h->tensors.data(), sizeof(ClipTensor) * h->tensors.size(),
-                   cudaMemcpyHostToDevice);
+  if (e == cudaSuccess) e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
+  if (e == cudaSuccess) e = cudaMemset(ws, 0, h->off_rows);   // counters, no tags
+  if (e == cudaSuccess && !h->rows.empty())
+    e = cudaMemcpy(ws + h->off_rows, h->rows.data(), sizeof(ClipRows) * h->rows.size(), cudaMemcpyHostToDevice);
+  if (e == cudaSuccess && !h->chunks.empty())
+    e = cudaMemcpy(ws + h->off_chunks, h->chunks.data(), sizeof(ClipChunk) * h->chunks.size(), cudaMemcpyHostToDevice);
   if (e == cudaSuccess) e = cudaDeviceSynchronize();
   if (e != cudaSuccess) return TOPOEP_ERR_CUDA;
+  long long ctas = (long long)kCtasPerSm * sms;
+  const long long wanted = ((long long)h->chunks.size() + kClipWarps - 1) / kClipWarps;
+  if (ctas > kMaxCtas) ctas = kMaxCtas;
+  if (ctas > wanted) ctas = wanted;
+  h->ctas = ctas < 1 ? 1 : (int)ctas;
   h->ws = ws;
   return TOPOEP_OK;
 }
@@ -214,21 +469,26 @@ static int enqueue_clip(topoep_clip_t h, int kind, float max_norm, float* dev_no
   if (!dev_norm) return TOPOEP_ERR_NULL;
   if (!aligned_to(dev_norm, 4)) return TOPOEP_ERR_ALIGN;
   ClipParams p = {};
-  p.tensors = reinterpret_cast<const ClipTensor*>(h->ws + h->off_tensors);
-  p.partial = reinterpret_cast<double*>(h->ws);
+  p.chunks = reinterpret_cast<const ClipChunk*>(h->ws + h->off_chunks);
+  p.rows = reinterpret_cast<const ClipRows*>(h->ws + h->off_rows);
+  p.partial = reinterpret_cast<ulonglong2*>(h->ws + h->off_partial);
+  p.control = reinterpret_cast<uint32_t*>(h->ws);
   p.norm = dev_norm;
-  p.chunks = h->chunks;
-  p.count = (int)h->tensors.size();
+  p.n_chunks = (long long)h->chunks.size();
+  p.keep_from = scale ? h->keep_from : p.n_chunks;
   p.kind = kind;
+  p.scale = scale;
   p.max_norm = max_norm;
-  long long blocks = 4ll * h->sms;
-  if (blocks > kMaxBlocks) blocks = kMaxBlocks;
-  if (blocks > h->chunks) blocks = h->chunks;
-  if (blocks < 1) blocks = 1;
-  p.blocks = (int)blocks;
-  clip_norm_kernel<<<(unsigned)blocks, kClipThreads, 0, stream>>>(p);
-  clip_scale_kernel<<<scale ? (unsigned)blocks : 1u, kClipThreads, 0, stream>>>(p, scale);
-  return cudaGetLastError() == cudaSuccess ? TOPOEP_OK : TOPOEP_ERR_CUDA;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(h->ctas);
+  cfg.blockDim = dim3(kClipThreads);
+  cfg.stream = stream;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeCooperative;   // the CTAs wait for one another's sums
+  attr[0].val.cooperative = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, clip_kernel, p) == cudaSuccess ? TOPOEP_OK : TOPOEP_ERR_CUDA;
 }
 
 extern "C" int topoep_clip_norm(topoep_clip_t h, int kind, float* dev_norm, topoep_stream_t stream) {

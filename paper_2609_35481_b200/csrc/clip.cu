@@ -61,13 +61,14 @@ struct ClipParams {
   uint32_t* control;       // serial number, CTAs that left, status
   float* norm;
   long long n_chunks, keep_from;
-  int kind, scale;
+  int scale;
   float max_norm;
 };
 enum { C_SERIAL = 0, C_LEAVE = 16, C_STATUS = 32 };
 
-__device__ __forceinline__ double join(double a, double b, int kind) {
-  if (kind == 0) return a + b;
+template <int KIND>
+__device__ __forceinline__ double join(double a, double b) {
+  if (KIND == 0) return a + b;
   return isnan(a) ? a : isnan(b) ? b : fmax(a, b);
 }
 
@@ -121,10 +122,10 @@ template <> struct Vec<__half> {
 };
 
 // What four vectors (or fewer: the rest are zero) add to the sum or maximum.
-template <typename T>
-__device__ __forceinline__ double take(const uint4 (&v)[4], int kind) {
+template <typename T, int KIND>
+__device__ __forceinline__ double take(const uint4 (&v)[4]) {
   constexpr int N = Vec<T>::N;
-  if (kind == 0) {
+  if (KIND == 0) {
     float s[N];
 #pragma unroll
     for (int i = 0; i < N; ++i) s[i] = 0.0f;
@@ -151,106 +152,140 @@ __device__ __forceinline__ double take(const uint4 (&v)[4], int kind) {
     }
     return d;
   }
-  double m = 0.0;
+  // |g| orders like its bits, and every NaN lies above infinity
+  uint32_t top = 0;
 #pragma unroll
   for (int q = 0; q < 4; ++q) {
-    float f[N], top = 0.0f;
+    float f[N];
     Vec<T>::get(v[q], f);
 #pragma unroll
-    for (int i = 0; i < N; ++i) top = fabsf(f[i]) <= top ? top : isnan(top) ? top : fabsf(f[i]);
-    m = join(m, top, 1);
+    for (int i = 0; i < N; ++i) top = max(top, __float_as_uint(f[i]) & 0x7fffffffu);
   }
-  return m;
+  return (double)__uint_as_float(top);
+}
+
+__device__ __forceinline__ float load_one(const char* p, int dtype) {
+  return dtype == TOPOEP_DTYPE_F32    ? *reinterpret_cast<const float*>(p)
+         : dtype == TOPOEP_DTYPE_BF16 ? to_f32(*reinterpret_cast<const __nv_bfloat16*>(p))
+                                      : to_f32(*reinterpret_cast<const __half*>(p));
+}
+__device__ __forceinline__ void store_one(char* p, int dtype, float v) {
+  if (dtype == TOPOEP_DTYPE_F32) *reinterpret_cast<float*>(p) = v;
+  else if (dtype == TOPOEP_DTYPE_BF16) *reinterpret_cast<__nv_bfloat16*>(p) = __float2bfloat16_rn(v);
+  else *reinterpret_cast<__half*>(p) = __float2half_rn(v);
+}
+
+template <int KIND>
+__device__ __forceinline__ double take_one(float v) {
+  const double g = (double)v;
+  return KIND == 0 ? g * g : fabs(g);
 }
 
 template <typename T>
-__device__ __forceinline__ double take_one(T v, int kind) {
-  const double g = (double)to_f32(v);
-  return kind == 0 ? g * g : fabs(g);
+__device__ __forceinline__ uint4 scaled(const uint4& v, float factor) {
+  float f[Vec<T>::N];
+  Vec<T>::get(v, f);
+#pragma unroll
+  for (int i = 0; i < Vec<T>::N; ++i) f[i] *= factor;
+  return Vec<T>::put(f);
 }
 
+// A chunk of adjacent elements: single ones up to the first 16-byte boundary, vectors, single ones.
+struct Body {
+  int head, vecs, tail, shift;   // tail: first element after the vectors; 2^shift bytes an element
+  __device__ __forceinline__ Body(const ClipChunk& c) {
+    shift = c.dtype == TOPOEP_DTYPE_F32 ? 2 : 1;
+    head = min(c.n, (int)((16 - (reinterpret_cast<uintptr_t>(c.src) & 15)) & 15) >> shift);
+    vecs = (c.n - head) >> (4 - shift);
+    tail = head + (vecs << (4 - shift));
+  }
+};
+
+// Element i of a tensor of short rows, in elements from its start.
 __device__ __forceinline__ long long offset_of(long long i, long long cols, long long stride) {
   return i / cols * stride + i % cols;
 }
 
-template <typename T>
-__device__ __forceinline__ double norm_chunk(const ClipParams& p, const ClipChunk& c, int kind, bool keep, int lane) {
+template <int KIND>
+__device__ __forceinline__ double norm_chunk(const ClipRows* rows, const ClipChunk& c, bool keep, int lane) {
+  const char* src = static_cast<const char*>(c.src);
+  const Body b(c);
   double sum = 0.0;
-  const T* src = static_cast<const T*>(c.src);
   if (c.tensor >= 0) {
-    const ClipRows r = p.rows[c.tensor];
+    const ClipRows r = rows[c.tensor];
     for (int i = lane; i < c.n; i += 32)
-      sum = join(sum, take_one(src[offset_of(c.first + i, r.cols, r.src_stride)], kind), kind);
+      sum = join<KIND>(sum, take_one<KIND>(load_one(src + (offset_of(c.first + i, r.cols, r.src_stride) << b.shift), c.dtype)));
     return sum;
   }
-  const int head = min(c.n, (int)(((16 - (reinterpret_cast<uintptr_t>(src) & 15)) & 15) / sizeof(T)));
-  const int vecs = (c.n - head) / Vec<T>::N, tail = head + vecs * Vec<T>::N;
-  if (lane < head) sum = take_one(src[lane], kind);
-  if (lane < c.n - tail) sum = join(sum, take_one(src[tail + lane], kind), kind);
-  const uint4* body = reinterpret_cast<const uint4*>(src + head);
-  for (int at = lane; at < vecs; at += 128) {
+  if (lane < b.head) sum = take_one<KIND>(load_one(src + (lane << b.shift), c.dtype));
+  if (lane < c.n - b.tail) sum = join<KIND>(sum, take_one<KIND>(load_one(src + ((b.tail + lane) << b.shift), c.dtype)));
+  const uint4* body = reinterpret_cast<const uint4*>(src + (b.head << b.shift));
+  for (int at = lane; at < b.vecs; at += 128) {
     uint4 v[4];
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
       v[q] = make_uint4(0, 0, 0, 0);
-      if (at + 32 * q < vecs) v[q] = keep ? __ldcg(body + at + 32 * q) : __ldcs(body + at + 32 * q);
+      if (at + 32 * q < b.vecs) v[q] = keep ? __ldcg(body + at + 32 * q) : __ldcs(body + at + 32 * q);
     }
-    sum = join(sum, take<T>(v, kind), kind);
+    sum = join<KIND>(sum, c.dtype == TOPOEP_DTYPE_BF16  ? take<__nv_bfloat16, KIND>(v)
+                          : c.dtype == TOPOEP_DTYPE_F32 ? take<float, KIND>(v)
+                                                        : take<__half, KIND>(v));
   }
   return sum;
 }
 
-template <typename T>
-__device__ __forceinline__ void scale_chunk(const ClipParams& p, const ClipChunk& c, float factor, int lane) {
-  const T* src = static_cast<const T*>(c.src);
-  T* dst = static_cast<T*>(c.dst);
+__device__ __forceinline__ void scale_chunk(const ClipRows* rows, const ClipChunk& c, float factor, int lane) {
+  const char* src = static_cast<const char*>(c.src);
+  char* dst = static_cast<char*>(c.dst);
+  const Body b(c);
   if (c.tensor >= 0) {
-    const ClipRows r = p.rows[c.tensor];
+    const ClipRows r = rows[c.tensor];
     for (int i = lane; i < c.n; i += 32)
-      dst[offset_of(c.first + i, r.cols, r.dst_stride)] =
-          from_f32<T>(to_f32(src[offset_of(c.first + i, r.cols, r.src_stride)]) * factor);
+      store_one(dst + (offset_of(c.first + i, r.cols, r.dst_stride) << b.shift), c.dtype,
+                load_one(src + (offset_of(c.first + i, r.cols, r.src_stride) << b.shift), c.dtype) * factor);
     return;
   }
   if (c.scalar) {
-    for (int i = lane; i < c.n; i += 32) dst[i] = from_f32<T>(to_f32(src[i]) * factor);
+    for (int i = lane; i < c.n; i += 32)
+      store_one(dst + (i << b.shift), c.dtype, load_one(src + (i << b.shift), c.dtype) * factor);
     return;
   }
-  const int head = min(c.n, (int)(((16 - (reinterpret_cast<uintptr_t>(src) & 15)) & 15) / sizeof(T)));
-  const int vecs = (c.n - head) / Vec<T>::N, tail = head + vecs * Vec<T>::N;
-  if (lane < head) dst[lane] = from_f32<T>(to_f32(src[lane]) * factor);
-  if (lane < c.n - tail) dst[tail + lane] = from_f32<T>(to_f32(src[tail + lane]) * factor);
-  const uint4* body = reinterpret_cast<const uint4*>(src + head);
-  uint4* out = reinterpret_cast<uint4*>(dst + head);
-  for (int at = lane; at < vecs; at += 128) {
+  if (lane < b.head) store_one(dst + (lane << b.shift), c.dtype, load_one(src + (lane << b.shift), c.dtype) * factor);
+  if (lane < c.n - b.tail) {
+    const int at = (b.tail + lane) << b.shift;
+    store_one(dst + at, c.dtype, load_one(src + at, c.dtype) * factor);
+  }
+  const uint4* body = reinterpret_cast<const uint4*>(src + (b.head << b.shift));
+  uint4* out = reinterpret_cast<uint4*>(dst + (b.head << b.shift));
+  for (int at = lane; at < b.vecs; at += 128) {
     uint4 v[4];
 #pragma unroll
     for (int q = 0; q < 4; ++q)
-      if (at + 32 * q < vecs) v[q] = __ldcs(body + at + 32 * q);
+      if (at + 32 * q < b.vecs) v[q] = __ldcs(body + at + 32 * q);
 #pragma unroll
     for (int q = 0; q < 4; ++q)
-      if (at + 32 * q < vecs) {
-        float f[Vec<T>::N];
-        Vec<T>::get(v[q], f);
-#pragma unroll
-        for (int i = 0; i < Vec<T>::N; ++i) f[i] *= factor;
-        __stcs(out + at + 32 * q, Vec<T>::put(f));
-      }
+      if (at + 32 * q < b.vecs)
+        __stcs(out + at + 32 * q, c.dtype == TOPOEP_DTYPE_BF16  ? scaled<__nv_bfloat16>(v[q], factor)
+                                  : c.dtype == TOPOEP_DTYPE_F32 ? scaled<float>(v[q], factor)
+                                                                : scaled<__half>(v[q], factor));
   }
 }
 
 // Sum (or maximum) over the block in a fixed order; valid in every thread.
-__device__ double block_join(double v, int kind, double* shared) {
+template <int KIND>
+__device__ double block_join(double v, double* shared) {
 #pragma unroll
-  for (int o = 16; o; o >>= 1) v = join(v, __shfl_xor_sync(0xffffffffu, v, o), kind);
+  for (int o = 16; o; o >>= 1) v = join<KIND>(v, __shfl_xor_sync(0xffffffffu, v, o));
   if ((threadIdx.x & 31) == 0) shared[threadIdx.x >> 5] = v;
   __syncthreads();
   v = (threadIdx.x & 31) < kClipWarps ? shared[threadIdx.x & 31] : 0.0;
 #pragma unroll
-  for (int o = 16; o; o >>= 1) v = join(v, __shfl_xor_sync(0xffffffffu, v, o), kind);
+  for (int o = 16; o; o >>= 1) v = join<KIND>(v, __shfl_xor_sync(0xffffffffu, v, o));
   __syncthreads();
   return v;
 }
 
+template <int KIND>
 __global__ void __launch_bounds__(kClipThreads, kCtasPerSm) clip_kernel(const ClipParams p) {
   __shared__ double shared[32];
   __shared__ int failed;
@@ -261,16 +296,14 @@ __global__ void __launch_bounds__(kClipThreads, kCtasPerSm) clip_kernel(const Cl
   if (threadIdx.x == 0) failed = 0;
 
   double sum = 0.0;
+  ClipChunk next = {};
+  if (warp < p.n_chunks) next = p.chunks[warp];
   for (long long i = warp; i < p.n_chunks; i += warps) {
-    const ClipChunk c = p.chunks[i];
-    const bool keep = i >= p.keep_from;
-    double v;
-    if (c.dtype == TOPOEP_DTYPE_BF16) v = norm_chunk<__nv_bfloat16>(p, c, p.kind, keep, lane);
-    else if (c.dtype == TOPOEP_DTYPE_F32) v = norm_chunk<float>(p, c, p.kind, keep, lane);
-    else v = norm_chunk<__half>(p, c, p.kind, keep, lane);
-    sum = join(sum, v, p.kind);
+    const ClipChunk c = next;
+    if (i + warps < p.n_chunks) next = p.chunks[i + warps];   // on its way while this one is read
+    sum = join<KIND>(sum, norm_chunk<KIND>(p.rows, c, i >= p.keep_from, lane));
   }
-  sum = block_join(sum, p.kind, shared);
+  sum = block_join<KIND>(sum, shared);
 
   const bool reads = p.scale || blockIdx.x == 0;
   if (gridDim.x > 1) {
@@ -291,21 +324,20 @@ __global__ void __launch_bounds__(kClipThreads, kCtasPerSm) clip_kernel(const Cl
         sum = __longlong_as_double((b << 32) | (a & 0xffffffffu));
         if (!got) { failed = 1; sum = __longlong_as_double(0x7ff8000000000000ll); }
       }
-      sum = block_join(sum, p.kind, shared);
+      sum = block_join<KIND>(sum, shared);
     }
   }
   if (reads) {
-    const float norm = (float)(p.kind == 0 ? sqrt(sum) : sum);
+    const float norm = (float)(KIND == 0 ? sqrt(sum) : sum);
     if (blockIdx.x == 0 && threadIdx.x == 0) *p.norm = norm;
     if (p.scale && !failed) {
       const float f = p.max_norm / (norm + kClipEps), factor = f > 1.0f ? 1.0f : f;   // a NaN stays
       const long long mine = warp < p.n_chunks ? (p.n_chunks - warp + warps - 1) / warps : 0;
-      for (long long k = mine; k-- > 0;) {
-        const ClipChunk c = p.chunks[warp + k * warps];
+      for (long long k = mine; k-- > 0;) {   // `next` still holds the last one
+        const ClipChunk c = next;
+        if (k > 0) next = p.chunks[warp + (k - 1) * warps];
         if (factor == 1.0f && c.dst == c.src) continue;
-        if (c.dtype == TOPOEP_DTYPE_BF16) scale_chunk<__nv_bfloat16>(p, c, factor, lane);
-        else if (c.dtype == TOPOEP_DTYPE_F32) scale_chunk<float>(p, c, factor, lane);
-        else scale_chunk<__half>(p, c, factor, lane);
+        scale_chunk(p.rows, c, factor, lane);
       }
     }
   }
@@ -476,7 +508,6 @@ static int enqueue_clip(topoep_clip_t h, int kind, float max_norm, float* dev_no
   p.norm = dev_norm;
   p.n_chunks = (long long)h->chunks.size();
   p.keep_from = scale ? h->keep_from : p.n_chunks;
-  p.kind = kind;
   p.scale = scale;
   p.max_norm = max_norm;
   cudaLaunchConfig_t cfg = {};
@@ -488,7 +519,8 @@ static int enqueue_clip(topoep_clip_t h, int kind, float max_norm, float* dev_no
   attr[0].val.cooperative = 1;
   cfg.attrs = attr;
   cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, clip_kernel, p) == cudaSuccess ? TOPOEP_OK : TOPOEP_ERR_CUDA;
+  const cudaError_t e = kind == 0 ? cudaLaunchKernelEx(&cfg, clip_kernel<0>, p) : cudaLaunchKernelEx(&cfg, clip_kernel<1>, p);
+  return e == cudaSuccess ? TOPOEP_OK : TOPOEP_ERR_CUDA;
 }
 
 extern "C" int topoep_clip_norm(topoep_clip_t h, int kind, float* dev_norm, topoep_stream_t stream) {

@@ -1,7 +1,8 @@
 // Router of an MoE layer: scores of a token's experts -> ids and weights of the chosen ones, and
 // the gradient of the scores.  The definitions stand in topoep.h.
-#include <cmath>
+#include <algorithm>
 #include <climits>
+#include <cmath>
 
 #include "layer_common.cuh"
 
@@ -23,6 +24,7 @@ struct RouterParams {
   long long stride, grad_stride, tokens;
   int E, k;
   float scale;
+  bool sigmoid, norm;
 };
 
 __device__ __forceinline__ float sigmoid_of(float l) { return 1.0f / (1.0f + expf(-l)); }
@@ -133,36 +135,252 @@ __global__ void __launch_bounds__(kRouterThreads) router_backward_any_kernel(con
   if (taken) grad[id] = from_f32<T>(part);
 }
 
+// ------------------------------------------------------------------ up to 512 experts, forward
+//
+// One warp a token, VPL logits in the registers of each lane, the next token's row on its way
+// meanwhile.  262144 tokens of 256 experts leave about 190 instructions a token at the speed of
+// the memory, so the choice is made in few of them:
+//   1. every lane's largest choice value; k rounds of a warp maximum give the k-th largest t of the
+//      32 lane maxima.  At least k values are >= t, so nothing below t is chosen, and seldom more
+//      than a few others are: about nine candidates for k = 8 of 256.
+//   2. the candidates' ids are compacted into shared memory, one a lane;
+//   3. a candidate's place is the number of candidates before it in (value, id) order, which it
+//      counts itself; the lanes with a place below k write it.
+// More than 32 candidates (many equal logits) take k rounds over the registers instead.
+
+template <typename T, int N> struct Row;   // N adjacent elements
+template <> struct Row<float, 1> { using type = float; };
+template <> struct Row<float, 2> { using type = float2; };
+template <> struct Row<float, 4> { using type = float4; };
+template <> struct Row<__nv_bfloat16, 1> { using type = __nv_bfloat16; };
+template <> struct Row<__nv_bfloat16, 2> { using type = uint32_t; };
+template <> struct Row<__nv_bfloat16, 4> { using type = uint2; };
+template <> struct Row<__nv_bfloat16, 8> { using type = uint4; };
+template <> struct Row<__half, 1> { using type = __half; };
+template <> struct Row<__half, 2> { using type = uint32_t; };
+template <> struct Row<__half, 4> { using type = uint2; };
+template <> struct Row<__half, 8> { using type = uint4; };
+
+// Lane's element i of a row is expert expert_of<W>(i, lane): vectors of W, lanes side by side.  Rows
+// that cannot be read as vectors are read element by element into the same places, so that the
+// order of every sum, and with it every bit, is the same.
+template <typename T, int VPL> constexpr int kVecOf = VPL * sizeof(T) <= 16 ? VPL : 16 / (int)sizeof(T);
+
+template <int W>
+__device__ __forceinline__ int expert_of(int i, int lane) { return i / W * (32 * W) + lane * W + i % W; }
+
+template <typename T, int VPL, bool VEC>
+__device__ __forceinline__ void load_row(const T* row, int E, int lane, float (&x)[VPL]) {
+  constexpr int W = kVecOf<T, VPL>;
+#pragma unroll
+  for (int v = 0; v < VPL / W; ++v) {
+    const int at = expert_of<W>(v * W, lane);
+    if (VEC && at < E) {   // E is a multiple of W
+      const typename Row<T, W>::type raw = *reinterpret_cast<const typename Row<T, W>::type*>(row + at);
+      const T* e = reinterpret_cast<const T*>(&raw);
+#pragma unroll
+      for (int i = 0; i < W; ++i) x[v * W + i] = to_f32(e[i]);
+    } else {
+#pragma unroll
+      for (int i = 0; i < W; ++i) x[v * W + i] = !VEC && at + i < E ? to_f32(row[at + i]) : -INFINITY;
+    }
+  }
+}
+
+__device__ __forceinline__ float warp_max(float v) {   // of the values that are not NaN
+  float r;
+  asm("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(r) : "f"(v));
+  return r;
+}
+
+// k rounds over the registers, any number of candidates: lane j returns the j-th choice.
+template <int VPL, int W>
+__device__ __noinline__ int choose_slowly(const float (&c)[VPL], int k, int lane) {
+  unsigned long long last = ~0ull;
+  int mine = -1;
+  for (int j = 0; j < k; ++j) {
+    unsigned long long best = 0;
+#pragma unroll
+    for (int i = 0; i < VPL; ++i) {
+      const unsigned key = order_key(c[i]);
+      const unsigned long long full = key ? ((unsigned long long)key << 32) | (0xffffffffu - expert_of<W>(i, lane)) : 0ull;
+      if (full < last && full > best) best = full;
+    }
+#pragma unroll
+    for (int o = 16; o; o >>= 1) {
+      const unsigned long long other = __shfl_xor_sync(0xffffffffu, best, o);
+      best = other > best ? other : best;
+    }
+    if (best == 0) break;
+    if (lane == j) mine = (int)(0xffffffffu - (unsigned)best);
+    last = best;
+  }
+  return mine;
+}
+
+template <typename T, int VPL, bool VEC>
+__global__ void __launch_bounds__(kRouterThreads) router_forward_kernel(const RouterParams p) {
+  constexpr int W = kVecOf<T, VPL>;
+  __shared__ float2 candidates[kRouterThreads / 32][32];   // choice value, then logit; id
+  const int lane = threadIdx.x & 31;
+  float2* cand = candidates[threadIdx.x >> 5];
+  const long long step = (long long)gridDim.x * (kRouterThreads / 32);
+  long long t = (long long)blockIdx.x * (kRouterThreads / 32) + (threadIdx.x >> 5);
+  if (t >= p.tokens) return;
+  const T* logits = static_cast<const T*>(p.logits);
+  float next[VPL];
+  load_row<T, VPL, VEC>(logits + t * p.stride, p.E, lane, next);
+  for (; t < p.tokens; t += step) {
+    const T* row = logits + t * p.stride;
+    float x[VPL];
+#pragma unroll
+    for (int i = 0; i < VPL; ++i) x[i] = next[i];
+    if (t + step < p.tokens) load_row<T, VPL, VEC>(row + step * p.stride, p.E, lane, next);
+    if (p.bias) {
+#pragma unroll
+      for (int i = 0; i < VPL; ++i) {
+        const int e = expert_of<W>(i, lane);
+        if (e < p.E && x[i] != -INFINITY) x[i] = sigmoid_of(x[i]) + __ldg(p.bias + e);
+      }
+    }
+    // comparisons with a NaN are false and a maximum passes it over: it is never a candidate
+    float most = x[0], at_least = -INFINITY, top = -INFINITY;
+#pragma unroll
+    for (int i = 1; i < VPL; ++i) most = fmaxf(most, x[i]);
+    most = fmaxf(most, -INFINITY);
+    if (VPL > 1) {
+      float left = most;
+      for (int j = 0; j < p.k; ++j) {
+        at_least = warp_max(left);
+        if (j == 0) top = at_least;
+        if (left == at_least) left = -INFINITY;
+      }
+    } else {
+      top = warp_max(most);
+    }
+    const bool masked = p.mask && p.mask[t] == 0;
+    unsigned mine = 0;
+#pragma unroll
+    for (int i = 0; i < VPL; ++i)
+      if (x[i] >= at_least && x[i] > -INFINITY) mine |= 1u << i;
+    if (masked) mine = 0;
+    const int n = __reduce_add_sync(0xffffffffu, __popc(mine));
+    int id = -1;
+    float z = 0.0f;
+    if (n <= 32) {
+      int base = 0;
+      __syncwarp();
+      for (unsigned some = __ballot_sync(0xffffffffu, mine != 0); some; some = __ballot_sync(0xffffffffu, mine != 0)) {
+        if (mine) {
+          cand[base + __popc(some & ((1u << lane) - 1))].y = __int_as_float(expert_of<W>(__ffs(mine) - 1, lane));
+          mine &= mine - 1;
+        }
+        base += __popc(some);
+      }
+      __syncwarp();
+      float c = -INFINITY;
+      if (lane < n) {
+        id = __float_as_int(cand[lane].y);
+        c = z = to_f32(row[id]);
+        if (p.bias) c = sigmoid_of(z) + __ldg(p.bias + id);
+        cand[lane].x = c;
+      }
+      __syncwarp();
+      int place = 0;
+      for (int j = 0; j < n; ++j) {
+        const float2 other = cand[j];
+        place += other.x > c || (other.x == c && __float_as_int(other.y) < id);
+      }
+      __syncwarp();
+      if (lane < n && place < p.k) cand[place] = make_float2(z, __int_as_float(id));
+      __syncwarp();
+      id = -1;
+      if (lane < min(n, p.k)) {   // lane j now has the j-th choice
+        z = cand[lane].x;
+        id = __float_as_int(cand[lane].y);
+      }
+    } else {
+      id = choose_slowly<VPL, W>(x, p.k, lane);
+      if (id >= 0) z = to_f32(row[id]);
+    }
+    float w = 0.0f;
+    if (p.sigmoid) {
+      if (id >= 0) w = sigmoid_of(z);
+      if (p.norm) w = w / (warp_sum(w) + kSigmoidEps);
+    } else {
+      if (id >= 0) w = expf(z - top);
+      float sum = w;
+      if (!p.norm) {   // over all experts
+        sum = 0.0f;
+#pragma unroll
+        for (int i = 0; i < VPL; ++i) sum += __expf(x[i] - top);
+      }
+      w = w / warp_sum(sum);
+    }
+    if (lane < p.k) {
+      p.ids[t * p.k + lane] = id;
+      p.weights[t * p.k + lane] = id >= 0 ? w * p.scale : 0.0f;
+    }
+  }
+}
+
+// Enough warps for every SM to be full, or one a token.
+unsigned router_blocks(long long tokens, int sms, int threads_per_token, int blocks_per_sm) {
+  const long long per = kRouterThreads / threads_per_token, wanted = (tokens + per - 1) / per;
+  return (unsigned)std::min(wanted, (long long)sms * blocks_per_sm);
+}
+
+template <typename T, int VPL>
+cudaError_t launch_forward_rows(const RouterParams& p, int sms, cudaStream_t stream) {
+  constexpr int W = kVecOf<T, VPL>;
+  const unsigned blocks = router_blocks(p.tokens, sms, 32, 2048 / kRouterThreads);
+  if (p.E % W == 0 && aligned_to(p.logits, W * sizeof(T)) && (p.tokens == 1 || p.stride % W == 0))
+    router_forward_kernel<T, VPL, true><<<blocks, kRouterThreads, 0, stream>>>(p);
+  else
+    router_forward_kernel<T, VPL, false><<<blocks, kRouterThreads, 0, stream>>>(p);
+  return cudaGetLastError();
+}
+
 template <typename T, bool SIGMOID, bool NORM>
-cudaError_t launch_forward(const RouterParams& p, cudaStream_t stream) {
+cudaError_t launch_forward(const RouterParams& p, int sms, cudaStream_t stream) {
+  if (p.E <= 32) return launch_forward_rows<T, 1>(p, sms, stream);
+  if (p.E <= 64) return launch_forward_rows<T, 2>(p, sms, stream);
+  if (p.E <= 128) return launch_forward_rows<T, 4>(p, sms, stream);
+  if (p.E <= 256) return launch_forward_rows<T, 8>(p, sms, stream);
+  if (p.E <= 512) return launch_forward_rows<T, 16>(p, sms, stream);
   const long long blocks = (p.tokens + kRouterThreads / 32 - 1) / (kRouterThreads / 32);
   router_forward_any_kernel<T, SIGMOID, NORM><<<(unsigned)blocks, kRouterThreads, 0, stream>>>(p);
   return cudaGetLastError();
 }
 
 template <typename T, bool SIGMOID, bool NORM>
-cudaError_t launch_backward(const RouterParams& p, cudaStream_t stream) {
+cudaError_t launch_backward(const RouterParams& p, int, cudaStream_t stream) {
   const long long blocks = (p.tokens + kRouterThreads / 32 - 1) / (kRouterThreads / 32);
   router_backward_any_kernel<T, SIGMOID, NORM><<<(unsigned)blocks, kRouterThreads, 0, stream>>>(p);
   return cudaGetLastError();
 }
 
 template <typename T>
-cudaError_t launch_typed(const RouterParams& p, bool sigmoid, bool norm, bool forward, cudaStream_t s) {
+cudaError_t launch_typed(const RouterParams& p, bool sigmoid, bool norm, bool forward, int sms, cudaStream_t s) {
   if (forward)
-    return sigmoid ? (norm ? launch_forward<T, true, true>(p, s) : launch_forward<T, true, false>(p, s))
-                   : (norm ? launch_forward<T, false, true>(p, s) : launch_forward<T, false, false>(p, s));
-  return sigmoid ? (norm ? launch_backward<T, true, true>(p, s) : launch_backward<T, true, false>(p, s))
-                 : (norm ? launch_backward<T, false, true>(p, s) : launch_backward<T, false, false>(p, s));
+    return sigmoid ? (norm ? launch_forward<T, true, true>(p, sms, s) : launch_forward<T, true, false>(p, sms, s))
+                   : (norm ? launch_forward<T, false, true>(p, sms, s) : launch_forward<T, false, false>(p, sms, s));
+  return sigmoid ? (norm ? launch_backward<T, true, true>(p, sms, s) : launch_backward<T, true, false>(p, sms, s))
+                 : (norm ? launch_backward<T, false, true>(p, sms, s) : launch_backward<T, false, false>(p, sms, s));
 }
 
-int launch(const topoep_router_config* cfg, const RouterParams& p, bool forward, cudaStream_t s) {
+int launch(const topoep_router_config* cfg, RouterParams& p, bool forward, cudaStream_t s) {
   const bool sigmoid = cfg->score == TOPOEP_SCORE_SIGMOID, norm = cfg->normalize != 0;
-  cudaError_t e;
+  p.sigmoid = sigmoid;
+  p.norm = norm;
+  int dev = 0, sms = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e == cudaSuccess) e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
+  if (e != cudaSuccess) return TOPOEP_ERR_CUDA;
   switch (cfg->dtype) {
-    case TOPOEP_DTYPE_F32: e = launch_typed<float>(p, sigmoid, norm, forward, s); break;
-    case TOPOEP_DTYPE_BF16: e = launch_typed<__nv_bfloat16>(p, sigmoid, norm, forward, s); break;
-    default: e = launch_typed<__half>(p, sigmoid, norm, forward, s); break;
+    case TOPOEP_DTYPE_F32: e = launch_typed<float>(p, sigmoid, norm, forward, sms, s); break;
+    case TOPOEP_DTYPE_BF16: e = launch_typed<__nv_bfloat16>(p, sigmoid, norm, forward, sms, s); break;
+    default: e = launch_typed<__half>(p, sigmoid, norm, forward, sms, s); break;
   }
   return e == cudaSuccess ? TOPOEP_OK : TOPOEP_ERR_CUDA;
 }

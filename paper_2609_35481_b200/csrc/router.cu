@@ -1,6 +1,7 @@
 // Router of an MoE layer: scores of a token's experts -> ids and weights of the chosen ones, and
 // the gradient of the scores.  The definitions stand in topoep.h.
 #include <algorithm>
+#include <cfloat>
 #include <climits>
 #include <cmath>
 
@@ -137,8 +138,7 @@ __global__ void __launch_bounds__(kRouterThreads) router_backward_any_kernel(con
 
 // ------------------------------------------------------------------ up to 512 experts, forward
 //
-// One warp a token, VPL logits in the registers of each lane, the next token's row on its way
-// meanwhile.  262144 tokens of 256 experts leave about 190 instructions a token at the speed of
+// One warp a token, VPL logits in the registers of each lane.  262144 tokens of 256 experts leave about 190 instructions a token at the speed of
 // the memory, so the choice is made in few of them:
 //   1. every lane's largest choice value; k rounds of a warp maximum give the k-th largest t of the
 //      32 lane maxima.  At least k values are >= t, so nothing below t is chosen, and seldom more
@@ -195,9 +195,10 @@ __device__ __forceinline__ float warp_max(float v) {   // of the values that are
 
 // k rounds over the registers, any number of candidates: lane j returns the j-th choice.
 template <int VPL, int W>
-__device__ __noinline__ int choose_slowly(const float (&c)[VPL], int k, int lane) {
+__device__ __forceinline__ int choose_slowly(const float (&c)[VPL], int k, int lane) {
   unsigned long long last = ~0ull;
   int mine = -1;
+#pragma unroll 1
   for (int j = 0; j < k; ++j) {
     unsigned long long best = 0;
 #pragma unroll
@@ -221,21 +222,19 @@ __device__ __noinline__ int choose_slowly(const float (&c)[VPL], int k, int lane
 template <typename T, int VPL, bool VEC>
 __global__ void __launch_bounds__(kRouterThreads) router_forward_kernel(const RouterParams p) {
   constexpr int W = kVecOf<T, VPL>;
-  __shared__ float2 candidates[kRouterThreads / 32][32];   // choice value, then logit; id
+  __shared__ __align__(16) float values[kRouterThreads / 32][32];   // of the candidates
+  __shared__ int numbers[kRouterThreads / 32][32];
   const int lane = threadIdx.x & 31;
-  float2* cand = candidates[threadIdx.x >> 5];
-  const long long step = (long long)gridDim.x * (kRouterThreads / 32);
+  float* value = values[threadIdx.x >> 5];
+  int* number = numbers[threadIdx.x >> 5];
+  const int step = gridDim.x * (kRouterThreads / 32), k = p.k;
   long long t = (long long)blockIdx.x * (kRouterThreads / 32) + (threadIdx.x >> 5);
-  if (t >= p.tokens) return;
-  const T* logits = static_cast<const T*>(p.logits);
-  float next[VPL];
-  load_row<T, VPL, VEC>(logits + t * p.stride, p.E, lane, next);
-  for (; t < p.tokens; t += step) {
-    const T* row = logits + t * p.stride;
+  const T* row = static_cast<const T*>(p.logits) + t * p.stride;
+  int32_t* out_id = p.ids + t * k + lane;
+  float* out_w = p.weights + t * k + lane;
+  for (; t < p.tokens; t += step, row += step * p.stride, out_id += step * k, out_w += step * k) {
     float x[VPL];
-#pragma unroll
-    for (int i = 0; i < VPL; ++i) x[i] = next[i];
-    if (t + step < p.tokens) load_row<T, VPL, VEC>(row + step * p.stride, p.E, lane, next);
+    load_row<T, VPL, VEC>(row, p.E, lane, x);
     if (p.bias) {
 #pragma unroll
       for (int i = 0; i < VPL; ++i) {
@@ -244,69 +243,75 @@ __global__ void __launch_bounds__(kRouterThreads) router_forward_kernel(const Ro
       }
     }
     // comparisons with a NaN are false and a maximum passes it over: it is never a candidate
-    float most = x[0], at_least = -INFINITY, top = -INFINITY;
+    float left = x[0], at_least = -INFINITY;
 #pragma unroll
-    for (int i = 1; i < VPL; ++i) most = fmaxf(most, x[i]);
-    most = fmaxf(most, -INFINITY);
+    for (int i = 1; i < VPL; ++i) left = fmaxf(left, x[i]);
+    const float top = warp_max(fmaxf(left, -INFINITY));
     if (VPL > 1) {
-      float left = most;
-      for (int j = 0; j < p.k; ++j) {
-        at_least = warp_max(left);
-        if (j == 0) top = at_least;
+      at_least = top;
+#pragma unroll 7
+      for (int j = 1; j < k; ++j) {
         if (left == at_least) left = -INFINITY;
+        at_least = warp_max(left);
       }
-    } else {
-      top = warp_max(most);
     }
-    const bool masked = p.mask && p.mask[t] == 0;
+    at_least = fmaxf(at_least, -FLT_MAX);   // -inf is no candidate
     unsigned mine = 0;
 #pragma unroll
     for (int i = 0; i < VPL; ++i)
-      if (x[i] >= at_least && x[i] > -INFINITY) mine |= 1u << i;
-    if (masked) mine = 0;
-    const int n = __reduce_add_sync(0xffffffffu, __popc(mine));
+      if (x[i] >= at_least) mine |= 1u << i;
+    if (p.mask && p.mask[t] == 0) mine = 0;
+    int n = 0;
+    value[lane] = -INFINITY;
+    for (unsigned some = __ballot_sync(0xffffffffu, mine != 0); some; some = __ballot_sync(0xffffffffu, mine != 0)) {
+      const int at = n + __popc(some & ((1u << lane) - 1));
+      if (mine && at < 32) number[at] = expert_of<W>(__ffs(mine) - 1, lane);
+      mine &= mine - 1;
+      n += __popc(some);
+    }
     int id = -1;
     float z = 0.0f;
+    __syncwarp();
     if (n <= 32) {
-      int base = 0;
-      __syncwarp();
-      for (unsigned some = __ballot_sync(0xffffffffu, mine != 0); some; some = __ballot_sync(0xffffffffu, mine != 0)) {
-        if (mine) {
-          cand[base + __popc(some & ((1u << lane) - 1))].y = __int_as_float(expert_of<W>(__ffs(mine) - 1, lane));
-          mine &= mine - 1;
-        }
-        base += __popc(some);
-      }
-      __syncwarp();
       float c = -INFINITY;
       if (lane < n) {
-        id = __float_as_int(cand[lane].y);
+        id = number[lane];
         c = z = to_f32(row[id]);
         if (p.bias) c = sigmoid_of(z) + __ldg(p.bias + id);
-        cand[lane].x = c;
+        value[lane] = c;
       }
       __syncwarp();
       int place = 0;
-      for (int j = 0; j < n; ++j) {
-        const float2 other = cand[j];
-        place += other.x > c || (other.x == c && __float_as_int(other.y) < id);
+      for (int j = 0; j < n; j += 4) {
+        const float4 other = *reinterpret_cast<const float4*>(value + j);
+        place += (other.x > c) + (other.y > c) + (other.z > c) + (other.w > c);
+      }
+      if (lane >= n) place = lane;
+      // equal values share a place and leave another empty: then ids count too
+      if (__reduce_or_sync(0xffffffffu, 1u << place) != 0xffffffffu && lane < n) {
+        place = 0;
+        for (int j = 0; j < n; ++j) place += value[j] > c || (value[j] == c && number[j] < id);
       }
       __syncwarp();
-      if (lane < n && place < p.k) cand[place] = make_float2(z, __int_as_float(id));
+      if (lane < n) {
+        value[place] = z;
+        number[place] = id;
+      }
       __syncwarp();
       id = -1;
-      if (lane < min(n, p.k)) {   // lane j now has the j-th choice
-        z = cand[lane].x;
-        id = __float_as_int(cand[lane].y);
+      if (lane < min(n, k)) {   // lane j now has the j-th choice
+        z = value[lane];
+        id = number[lane];
       }
+      __syncwarp();
     } else {
-      id = choose_slowly<VPL, W>(x, p.k, lane);
+      id = choose_slowly<VPL, W>(x, k, lane);
       if (id >= 0) z = to_f32(row[id]);
     }
     float w = 0.0f;
     if (p.sigmoid) {
       if (id >= 0) w = sigmoid_of(z);
-      if (p.norm) w = w / (warp_sum(w) + kSigmoidEps);
+      if (p.norm) w = __fdividef(w, warp_sum(w) + kSigmoidEps);
     } else {
       if (id >= 0) w = expf(z - top);
       float sum = w;
@@ -315,11 +320,11 @@ __global__ void __launch_bounds__(kRouterThreads) router_forward_kernel(const Ro
 #pragma unroll
         for (int i = 0; i < VPL; ++i) sum += __expf(x[i] - top);
       }
-      w = w / warp_sum(sum);
+      w = __fdividef(w, warp_sum(sum));
     }
-    if (lane < p.k) {
-      p.ids[t * p.k + lane] = id;
-      p.weights[t * p.k + lane] = id >= 0 ? w * p.scale : 0.0f;
+    if (lane < k) {
+      *out_id = id;
+      *out_w = id >= 0 ? w * p.scale : 0.0f;
     }
   }
 }

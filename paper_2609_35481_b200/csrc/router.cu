@@ -12,6 +12,11 @@ namespace topoep {
 namespace {
 
 constexpr int kRouterThreads = 128;
+constexpr int kRouterBlocksPerSm = 8, kBackwardBlocksPerSm = 12, kSparseBlocksPerSm = 12;
+// Up to so many tokens an SM a whole warp takes a token, beyond that eight lanes do (more than 64
+// experts): 4096 tokens of 256 experts 4.4 against 4.1 us, with a bias 5.3 against 7.8; one token 3.1
+// against 3.3, with a bias 3.6 against 6.7; 16384 tokens 12.9 against 7.7.
+constexpr int kFew = 32;
 constexpr float kSigmoidEps = 1e-20f;
 
 struct RouterParams {
@@ -28,7 +33,7 @@ struct RouterParams {
   bool sigmoid, norm;
 };
 
-__device__ __forceinline__ float sigmoid_of(float l) { return 1.0f / (1.0f + expf(-l)); }
+__device__ __forceinline__ float sigmoid_of(float l) { return __frcp_rn(1.0f + expf(-l)); }
 
 // Orders floats like unsigned integers; what may never be chosen (-inf, NaN) is 0.
 __device__ __forceinline__ unsigned order_key(float c) {
@@ -102,7 +107,9 @@ __global__ void __launch_bounds__(kRouterThreads) router_forward_any_kernel(cons
   }
 }
 
-template <typename T, bool SIGMOID, bool NORM>
+// Gradient through the softmax over any number of experts: one warp a token, the row read from
+// L1/L2 after the first time.
+template <typename T>
 __global__ void __launch_bounds__(kRouterThreads) router_backward_any_kernel(const RouterParams p) {
   const int lane = threadIdx.x & 31;
   const long long t = (long long)blockIdx.x * (kRouterThreads / 32) + (threadIdx.x >> 5);
@@ -113,40 +120,38 @@ __global__ void __launch_bounds__(kRouterThreads) router_backward_any_kernel(con
   if (id >= p.E) id = -1;
   const bool taken = id >= 0;
   const float w = taken ? p.weights[t * p.k + lane] : 0.0f;
-  const float dw = taken ? p.grad_weights[t * p.k + lane] : 0.0f;
-  const float wdw = w * dw;
-  const float m = warp_sum(wdw) / p.scale;
-  float part = NORM ? w * (dw - m) : wdw;
-  if (SIGMOID && taken) part = part / (1.0f + expf(to_f32(row[id])));
-  if (!SIGMOID && !NORM && __any_sync(0xffffffffu, taken)) {
-    float top = -INFINITY;
+  const float wdw = taken ? w * p.grad_weights[t * p.k + lane] : 0.0f;
+  const float all = warp_sum(wdw);
+  float c = 0.0f, top = -INFINITY;
+  const bool any = __any_sync(0xffffffffu, taken);
+  if (any) {
     for (int i = lane; i < p.E; i += 32) top = fmaxf(top, to_f32(row[i]));
 #pragma unroll
     for (int o = 16; o; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
     float sum = 0.0f;
     for (int i = lane; i < p.E; i += 32) sum += expf(to_f32(row[i]) - top);
-    sum = warp_sum(sum);
-    const float c = -m * p.scale / sum;
-    for (int i = lane; i < p.E; i += 32) grad[i] = from_f32<T>(expf(to_f32(row[i]) - top) * c);
-    if (taken) part += expf(to_f32(row[id]) - top) * c;
-  } else {
-    for (int i = lane; i < p.E; i += 32) grad[i] = from_f32<T>(0.0f);
+    c = -all / warp_sum(sum);
   }
+  for (int i = lane; i < p.E; i += 32) grad[i] = from_f32<T>(any ? expf(to_f32(row[i]) - top) * c : 0.0f);
   __syncwarp();   // the chosen places are written after the row
-  if (taken) grad[id] = from_f32<T>(part);
+  if (taken) grad[id] = from_f32<T>(wdw - w * (all / p.scale));   // p_j = w_j / scale
 }
 
-// ------------------------------------------------------------------ up to 512 experts, forward
+// ----------------------------------------------------------------- up to 1024 experts, forward
 //
-// One warp a token, VPL logits in the registers of each lane.  262144 tokens of 256 experts leave about 190 instructions a token at the speed of
-// the memory, so the choice is made in few of them:
-//   1. every lane's largest choice value; k rounds of a warp maximum give the k-th largest t of the
-//      32 lane maxima.  At least k values are >= t, so nothing below t is chosen, and seldom more
-//      than a few others are: about nine candidates for k = 8 of 256.
-//   2. the candidates' ids are compacted into shared memory, one a lane;
-//   3. a candidate's place is the number of candidates before it in (value, id) order, which it
-//      counts itself; the lanes with a place below k write it.
-// More than 32 candidates (many equal logits) take k rounds over the registers instead.
+// 262144 tokens of 256 experts leave about 190 instructions a token at the speed of the memory, and
+// choosing 8 of 256 is a handful of values: with a warp a token most lanes idle (361 instructions,
+// 120 us).  So G = 8 lanes (16, 32 for more than 256, 512 experts) share a token, a warp works on
+// four, and each lane holds up to 32 logits in registers:
+//   1. each lane's logits in four groups, the group maxima sorted; k rounds of a maximum over the
+//      lanes' heads, the winner moving up its next, give the k-th largest t of the 4 G group maxima.
+//      At least k values are >= t, so nothing below t is chosen, and seldom more than a few others
+//      are (about nine candidates for k = 8 of 256).
+//   2. the candidates' ids are compacted into shared memory;
+//   3. a candidate's place is the number of larger candidates.  Equal values share a place, which
+//      the sum of the places gives away: then ids are compared too.
+// More than kCandidates of them (many equal logits) take k rounds over the rows instead.
+constexpr int kCandidates = 32;
 
 template <typename T, int N> struct Row;   // N adjacent elements
 template <> struct Row<float, 1> { using type = float; };
@@ -161,170 +166,359 @@ template <> struct Row<__half, 2> { using type = uint32_t; };
 template <> struct Row<__half, 4> { using type = uint2; };
 template <> struct Row<__half, 8> { using type = uint4; };
 
-// Lane's element i of a row is expert expert_of<W>(i, lane): vectors of W, lanes side by side.  Rows
-// that cannot be read as vectors are read element by element into the same places, so that the
+// Element i of lane `sub` of a token is expert expert_of(i, sub): vectors of W, lanes side by side.
+// Rows that cannot be read as vectors are read element by element into the same places, so that the
 // order of every sum, and with it every bit, is the same.
 template <typename T, int VPL> constexpr int kVecOf = VPL * sizeof(T) <= 16 ? VPL : 16 / (int)sizeof(T);
+template <int G, int W>
+__device__ __forceinline__ int expert_of(int i, int sub) { return i / W * (G * W) + sub * W + i % W; }
 
-template <int W>
-__device__ __forceinline__ int expert_of(int i, int lane) { return i / W * (32 * W) + lane * W + i % W; }
-
-template <typename T, int VPL, bool VEC>
-__device__ __forceinline__ void load_row(const T* row, int E, int lane, float (&x)[VPL]) {
+template <typename T, int G, int VPL, bool VEC>
+__device__ __forceinline__ void load_row(const T* row, int E, int sub, float (&x)[VPL]) {
   constexpr int W = kVecOf<T, VPL>;
+  if (VEC && E == G * VPL) {
 #pragma unroll
-  for (int v = 0; v < VPL / W; ++v) {
-    const int at = expert_of<W>(v * W, lane);
-    if (VEC && at < E) {   // E is a multiple of W
-      const typename Row<T, W>::type raw = *reinterpret_cast<const typename Row<T, W>::type*>(row + at);
+    for (int v = 0; v < VPL / W; ++v) {
+      const typename Row<T, W>::type raw = *reinterpret_cast<const typename Row<T, W>::type*>(row + expert_of<G, W>(v * W, sub));
       const T* e = reinterpret_cast<const T*>(&raw);
 #pragma unroll
       for (int i = 0; i < W; ++i) x[v * W + i] = to_f32(e[i]);
+    }
+    return;
+  }
+#pragma unroll
+  for (int v = 0; v < VPL / W; ++v) {
+    const int at = expert_of<G, W>(v * W, sub);
+    if (VEC) {   // E is a multiple of W
+      typename Row<T, W>::type raw;
+      if (at < E) raw = *reinterpret_cast<const typename Row<T, W>::type*>(row + at);
+      const T* e = reinterpret_cast<const T*>(&raw);
+#pragma unroll
+      for (int i = 0; i < W; ++i) x[v * W + i] = at < E ? to_f32(e[i]) : -INFINITY;
     } else {
 #pragma unroll
-      for (int i = 0; i < W; ++i) x[v * W + i] = !VEC && at + i < E ? to_f32(row[at + i]) : -INFINITY;
+      for (int i = 0; i < W; ++i) x[v * W + i] = at + i < E ? to_f32(row[at + i]) : -INFINITY;
     }
   }
 }
 
-__device__ __forceinline__ float warp_max(float v) {   // of the values that are not NaN
-  float r;
-  asm("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(r) : "f"(v));
-  return r;
+// Sum and maximum over the G lanes of a token.
+template <int G>
+__device__ __forceinline__ float lanes_sum(float v) {
+#pragma unroll
+  for (int o = G / 2; o; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+  return v;
+}
+template <int G>
+__device__ __forceinline__ float lanes_max(float v) {
+#pragma unroll
+  for (int o = G / 2; o; o >>= 1) v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, o));
+  return v;
 }
 
-// k rounds over the registers, any number of candidates: lane j returns the j-th choice.
-template <int VPL, int W>
-__device__ __forceinline__ int choose_slowly(const float (&c)[VPL], int k, int lane) {
-  unsigned long long last = ~0ull;
-  int mine = -1;
-#pragma unroll 1
-  for (int j = 0; j < k; ++j) {
-    unsigned long long best = 0;
-#pragma unroll
-    for (int i = 0; i < VPL; ++i) {
-      const unsigned key = order_key(c[i]);
-      const unsigned long long full = key ? ((unsigned long long)key << 32) | (0xffffffffu - expert_of<W>(i, lane)) : 0ull;
-      if (full < last && full > best) best = full;
-    }
-#pragma unroll
-    for (int o = 16; o; o >>= 1) {
-      const unsigned long long other = __shfl_xor_sync(0xffffffffu, best, o);
-      best = other > best ? other : best;
-    }
-    if (best == 0) break;
-    if (lane == j) mine = (int)(0xffffffffu - (unsigned)best);
-    last = best;
-  }
-  return mine;
+__device__ __forceinline__ void larger_first(float& a, float& b) {
+  const float hi = fmaxf(a, b);
+  b = fminf(a, b);
+  a = hi;
 }
 
-template <typename T, int VPL, bool VEC>
-__global__ void __launch_bounds__(kRouterThreads) router_forward_kernel(const RouterParams p) {
-  constexpr int W = kVecOf<T, VPL>;
-  __shared__ __align__(16) float values[kRouterThreads / 32][32];   // of the candidates
-  __shared__ int numbers[kRouterThreads / 32][32];
-  const int lane = threadIdx.x & 31;
-  float* value = values[threadIdx.x >> 5];
-  int* number = numbers[threadIdx.x >> 5];
-  const int step = gridDim.x * (kRouterThreads / 32), k = p.k;
-  long long t = (long long)blockIdx.x * (kRouterThreads / 32) + (threadIdx.x >> 5);
-  const T* row = static_cast<const T*>(p.logits) + t * p.stride;
-  int32_t* out_id = p.ids + t * k + lane;
-  float* out_w = p.weights + t * k + lane;
-  for (; t < p.tokens; t += step, row += step * p.stride, out_id += step * k, out_w += step * k) {
+struct Candidates {   // of one token
+  float value[kCandidates + 4];
+  float logit[kCandidates];
+  int number[kCandidates];
+  float out_logit[kCandidates];
+  int out_number[kCandidates];
+};
+
+template <typename T, int G, int VPL, bool VEC, bool BIAS>
+__global__ void __launch_bounds__(kRouterThreads, kRouterBlocksPerSm) router_forward_kernel(const RouterParams p) {
+  constexpr int W = kVecOf<T, VPL>, kTokens = 32 / G, kOuts = kCandidates / G;
+  __shared__ __align__(16) Candidates shared[kRouterThreads / G];
+  const int lane = threadIdx.x & 31, sub = lane & (G - 1), k = p.k;
+  Candidates& cand = shared[threadIdx.x / G];
+  const long long step = (long long)gridDim.x * (kRouterThreads / G);
+  long long first = (long long)blockIdx.x * (kRouterThreads / G) + (threadIdx.x >> 5) * kTokens;
+  for (; first < p.tokens; first += step) {
+    // lanes of a token past the last one repeat it and write nothing
+    const long long token = first + lane / G, t = min(token, p.tokens - 1);
+    const T* row = static_cast<const T*>(p.logits) + t * p.stride;
     float x[VPL];
-    load_row<T, VPL, VEC>(row, p.E, lane, x);
-    if (p.bias) {
+    load_row<T, G, VPL, VEC>(row, p.E, sub, x);
+    if (BIAS) {
 #pragma unroll
-      for (int i = 0; i < VPL; ++i) {
-        const int e = expert_of<W>(i, lane);
-        if (e < p.E && x[i] != -INFINITY) x[i] = sigmoid_of(x[i]) + __ldg(p.bias + e);
+      for (int v = 0; v < VPL; v += W) {
+        const int e = expert_of<G, W>(v, sub);
+        float b[W];
+#pragma unroll
+        for (int i = 0; i < W; ++i) b[i] = 0.0f;
+        if (VEC && W % 4 == 0 && e < p.E) {
+#pragma unroll
+          for (int i = 0; i < W; i += 4) {
+            const float4 f = __ldg(reinterpret_cast<const float4*>(p.bias + e + i));
+            b[i] = f.x; b[i + 1] = f.y; b[i + 2] = f.z; b[i + 3] = f.w;
+          }
+        } else {
+#pragma unroll
+          for (int i = 0; i < W; ++i)
+            if (e + i < p.E) b[i] = __ldg(p.bias + e + i);
+        }
+#pragma unroll
+        for (int i = 0; i < W; ++i)
+          if (x[v + i] != -INFINITY) x[v + i] = __fdividef(1.0f, 1.0f + __expf(-x[v + i])) + b[i];
       }
     }
     // comparisons with a NaN are false and a maximum passes it over: it is never a candidate
-    float left = x[0], at_least = -INFINITY;
+    float m[4];
 #pragma unroll
-    for (int i = 1; i < VPL; ++i) left = fmaxf(left, x[i]);
-    const float top = warp_max(fmaxf(left, -INFINITY));
-    if (VPL > 1) {
-      at_least = top;
-#pragma unroll 7
-      for (int j = 1; j < k; ++j) {
-        if (left == at_least) left = -INFINITY;
-        at_least = warp_max(left);
-      }
+    for (int g = 0; g < 4; ++g) {
+      m[g] = -INFINITY;
+#pragma unroll
+      for (int i = 0; i < VPL / 4; ++i) m[g] = fmaxf(m[g], x[g * (VPL / 4) + i]);
     }
+    larger_first(m[0], m[1]);
+    larger_first(m[2], m[3]);
+    larger_first(m[0], m[2]);
+    larger_first(m[1], m[3]);
+    larger_first(m[1], m[2]);
+    const float top = lanes_max<G>(m[0]);
+    float at_least = top;
+#pragma unroll 4
+    for (int j = 1; j < k; ++j) {
+      if (m[0] == at_least) { m[0] = m[1]; m[1] = m[2]; m[2] = m[3]; m[3] = -INFINITY; }
+      at_least = lanes_max<G>(m[0]);
+    }
+    // Up to here a biased score was formed with the fast exponential and reciprocal, within 2^-20 of
+    // the exact sigmoid; the candidates' are exact, so t is lowered by more than both errors.
+    if (BIAS) at_least -= 4e-6f + 5e-7f * fabsf(at_least);
     at_least = fmaxf(at_least, -FLT_MAX);   // -inf is no candidate
     unsigned mine = 0;
 #pragma unroll
     for (int i = 0; i < VPL; ++i)
       if (x[i] >= at_least) mine |= 1u << i;
     if (p.mask && p.mask[t] == 0) mine = 0;
-    int n = 0;
-    value[lane] = -INFINITY;
-    for (unsigned some = __ballot_sync(0xffffffffu, mine != 0); some; some = __ballot_sync(0xffffffffu, mine != 0)) {
-      const int at = n + __popc(some & ((1u << lane) - 1));
-      if (mine && at < 32) number[at] = expert_of<W>(__ffs(mine) - 1, lane);
-      mine &= mine - 1;
-      n += __popc(some);
-    }
-    int id = -1;
-    float z = 0.0f;
-    __syncwarp();
-    if (n <= 32) {
-      float c = -INFINITY;
-      if (lane < n) {
-        id = number[lane];
-        c = z = to_f32(row[id]);
-        if (p.bias) c = sigmoid_of(z) + __ldg(p.bias + id);
-        value[lane] = c;
-      }
-      __syncwarp();
-      int place = 0;
-      for (int j = 0; j < n; j += 4) {
-        const float4 other = *reinterpret_cast<const float4*>(value + j);
-        place += (other.x > c) + (other.y > c) + (other.z > c) + (other.w > c);
-      }
-      if (lane >= n) place = lane;
-      // equal values share a place and leave another empty: then ids count too
-      if (__reduce_or_sync(0xffffffffu, 1u << place) != 0xffffffffu && lane < n) {
-        place = 0;
-        for (int j = 0; j < n; ++j) place += value[j] > c || (value[j] == c && number[j] < id);
-      }
-      __syncwarp();
-      if (lane < n) {
-        value[place] = z;
-        number[place] = id;
-      }
-      __syncwarp();
-      id = -1;
-      if (lane < min(n, k)) {   // lane j now has the j-th choice
-        z = value[lane];
-        id = number[lane];
-      }
-      __syncwarp();
-    } else {
-      id = choose_slowly<VPL, W>(x, k, lane);
-      if (id >= 0) z = to_f32(row[id]);
-    }
-    float w = 0.0f;
-    if (p.sigmoid) {
-      if (id >= 0) w = sigmoid_of(z);
-      if (p.norm) w = __fdividef(w, warp_sum(w) + kSigmoidEps);
-    } else {
-      if (id >= 0) w = expf(z - top);
-      float sum = w;
-      if (!p.norm) {   // over all experts
-        sum = 0.0f;
+    int upto = __popc(mine);   // candidates of this lane and the ones before it
+    int at = -upto;
 #pragma unroll
-        for (int i = 0; i < VPL; ++i) sum += __expf(x[i] - top);
-      }
-      w = __fdividef(w, warp_sum(sum));
+    for (int o = 1; o < G; o <<= 1) {
+      const int v = __shfl_up_sync(0xffffffffu, upto, o, G);
+      if (sub >= o) upto += v;
     }
-    if (lane < k) {
-      *out_id = id;
-      *out_w = id >= 0 ? w * p.scale : 0.0f;
+    at += upto;
+    int n = __shfl_sync(0xffffffffu, upto, G - 1, G);
+    if (!__any_sync(0xffffffffu, n > kCandidates)) {
+      for (; mine; mine &= mine - 1) cand.number[at++] = expert_of<G, W>(__ffs(mine) - 1, sub);
+      __syncwarp();
+      for (int a = sub; a < n; a += G) {
+        const int id = cand.number[a];
+        const float z = to_f32(row[id]);
+        cand.logit[a] = z;
+        cand.value[a] = BIAS ? sigmoid_of(z) + __ldg(p.bias + id) : z;
+      }
+      if (sub < 4) cand.value[n + sub] = -INFINITY;   // read in fours
+      __syncwarp();
+      int places = 0;
+      for (int a = sub; a < n; a += G) {
+        const float c = cand.value[a];
+        int place = 0;
+        for (int j = 0; j < n; j += 4) {
+          const float4 o = *reinterpret_cast<const float4*>(cand.value + j);
+          place += (o.x > c) + (o.y > c) + (o.z > c) + (o.w > c);
+        }
+        places += place;
+        cand.out_logit[place] = cand.logit[a];
+        cand.out_number[place] = cand.number[a];
+      }
+#pragma unroll
+      for (int o = G / 2; o; o >>= 1) places += __shfl_xor_sync(0xffffffffu, places, o);
+      if (places != n * (n - 1) / 2) {   // equal values
+        for (int a = sub; a < n; a += G) {
+          const float c = cand.value[a];
+          const int id = cand.number[a];
+          int place = 0;
+          for (int j = 0; j < n; ++j) place += cand.value[j] > c || (cand.value[j] == c && cand.number[j] < id);
+          cand.out_logit[place] = cand.logit[a];
+          cand.out_number[place] = id;
+        }
+      }
+      __syncwarp();
+    } else {   // k rounds over the rows in L1, for all tokens of the warp
+      const bool left_out = n == 0;
+      unsigned long long last = ~0ull;
+      n = 0;
+#pragma unroll 1
+      for (int j = 0; j < k; ++j) {
+        unsigned long long best = 0;
+#pragma unroll 1
+        for (int e = sub; e < p.E; e += G) {
+          const float z = to_f32(row[e]);
+          unsigned key = order_key(z);
+          if (BIAS && key) key = order_key(sigmoid_of(z) + __ldg(p.bias + e));
+          const unsigned long long full = key ? ((unsigned long long)key << 32) | (0xffffffffu - e) : 0ull;
+          if (full < last && full > best) best = full;
+        }
+#pragma unroll
+        for (int o = G / 2; o; o >>= 1) {
+          const unsigned long long other = __shfl_xor_sync(0xffffffffu, best, o);
+          best = other > best ? other : best;
+        }
+        last = best;
+        if (best != 0 && !left_out) {
+          if (sub == 0) {
+            const int id = (int)(0xffffffffu - (unsigned)best);
+            cand.out_number[j] = id;
+            cand.out_logit[j] = to_f32(row[id]);
+          }
+          n = j + 1;
+        }
+      }
+      __syncwarp();
+    }
+    // lane `sub` has the choices sub, sub + G, ...
+    float w[kOuts], sum = 0.0f;
+#pragma unroll
+    for (int i = 0; i < kOuts; ++i) {
+      const int j = i * G + sub;
+      w[i] = 0.0f;
+      if (i * G >= k) break;
+      if (j < min(n, k)) {
+        const float z = cand.out_logit[j];
+        w[i] = p.sigmoid ? sigmoid_of(z) : expf(z - top);
+      }
+      sum += w[i];
+    }
+    if (!p.sigmoid && !p.norm) {   // over all experts
+      sum = 0.0f;
+#pragma unroll
+      for (int i = 0; i < VPL; ++i) sum += __expf(x[i] - top);
+    }
+    if (!p.sigmoid || p.norm) sum = lanes_sum<G>(sum) + (p.sigmoid ? kSigmoidEps : 0.0f);
+    else sum = 1.0f;
+#pragma unroll
+    for (int i = 0; i < kOuts; ++i) {
+      const int j = i * G + sub;
+      if (i * G >= k) break;
+      if (j < k && token < p.tokens) {
+        const bool taken = j < n;
+        p.ids[t * k + j] = taken ? cand.out_number[j] : -1;
+        p.weights[t * k + j] = taken ? __fdividef(w[i], sum) * p.scale : 0.0f;
+      }
+    }
+    __syncwarp();
+  }
+}
+
+// ---------------------------------------------------------------------------------- backward
+//
+// Bound by memory: a row of gradients written for each token and 12 bytes read for each choice; the
+// row of logits is read too where the softmax over all experts is differentiated, else only the
+// chosen logits.  The row goes out as vectors, then the chosen places are written over it.
+
+// Gradient at the chosen places only: eight lanes a token.  The zeros leave while the ids, weights
+// and their gradients are on their way.
+template <typename T, bool VEC>
+__global__ void __launch_bounds__(kRouterThreads, kSparseBlocksPerSm) router_backward_sparse_kernel(const RouterParams p) {
+  constexpr int G = 8, W = VEC ? 16 / (int)sizeof(T) : 1, kOuts = 32 / G;
+  const int lane = threadIdx.x & 31, sub = lane & (G - 1), k = p.k;
+  const long long step = (long long)gridDim.x * (kRouterThreads / G);
+  long long first = (long long)blockIdx.x * (kRouterThreads / G) + (threadIdx.x >> 5) * (32 / G);
+  for (; first < p.tokens; first += step) {
+    const long long token = first + lane / G, t = min(token, p.tokens - 1);
+    const bool mine = token < p.tokens;
+    const T* row = static_cast<const T*>(p.logits) + t * p.stride;
+    T* grad = static_cast<T*>(p.grad) + t * p.grad_stride;
+    int id[kOuts];
+    float w[kOuts], dw[kOuts], z[kOuts], sum = 0.0f;
+#pragma unroll
+    for (int i = 0; i < kOuts; ++i) {
+      if (i * G >= k) break;
+      const int j = i * G + sub;
+      id[i] = j < k ? p.ids[t * k + j] : -1;
+      w[i] = j < k ? p.weights[t * k + j] : 0.0f;
+      dw[i] = j < k ? p.grad_weights[t * k + j] : 0.0f;
+    }
+    if (mine) {
+      for (int at = sub * W; at < p.E; at += G * W) {
+        if (VEC) *reinterpret_cast<uint4*>(grad + at) = make_uint4(0, 0, 0, 0);
+        else grad[at] = from_f32<T>(0.0f);
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < kOuts; ++i) {
+      if (i * G >= k) break;
+      if (id[i] >= p.E) id[i] = -1;
+      z[i] = id[i] >= 0 && p.sigmoid ? to_f32(row[id[i]]) : 0.0f;
+      sum += id[i] >= 0 ? w[i] * dw[i] : 0.0f;
+    }
+    const float m = p.norm ? lanes_sum<G>(sum) / p.scale : 0.0f;
+    __syncwarp();   // the chosen places are written after the row
+#pragma unroll
+    for (int i = 0; i < kOuts; ++i) {
+      if (i * G >= k) break;
+      if (id[i] < 0 || !mine) continue;
+      float g = w[i] * (dw[i] - m);
+      if (p.sigmoid) g = g / (1.0f + expf(z[i]));
+      grad[id[i]] = from_f32<T>(g);
+    }
+  }
+}
+
+// Softmax over all experts, up to 1024: G lanes a token with the row in registers.
+template <typename T, int G, int VPL, bool VEC>
+__global__ void __launch_bounds__(kRouterThreads, kBackwardBlocksPerSm) router_backward_all_kernel(const RouterParams p) {
+  constexpr int W = kVecOf<T, VPL>, kTokens = 32 / G, kOuts = 32 / G;
+  const int lane = threadIdx.x & 31, sub = lane & (G - 1), k = p.k;
+  const long long step = (long long)gridDim.x * (kRouterThreads / G);
+  long long first = (long long)blockIdx.x * (kRouterThreads / G) + (threadIdx.x >> 5) * kTokens;
+  for (; first < p.tokens; first += step) {
+    const long long token = first + lane / G, t = min(token, p.tokens - 1);
+    const bool mine = token < p.tokens;
+    T* grad = static_cast<T*>(p.grad) + t * p.grad_stride;
+    float x[VPL];
+    load_row<T, G, VPL, VEC>(static_cast<const T*>(p.logits) + t * p.stride, p.E, sub, x);
+    int id[kOuts];
+    float wdw[kOuts], w[kOuts], sum = 0.0f;
+    bool any = false;
+#pragma unroll
+    for (int i = 0; i < kOuts; ++i) {
+      if (i * G >= k) break;
+      const int j = i * G + sub;
+      id[i] = j < k ? p.ids[t * k + j] : -1;
+      w[i] = j < k ? p.weights[t * k + j] : 0.0f;
+      wdw[i] = j < k ? w[i] * p.grad_weights[t * k + j] : 0.0f;
+      if (id[i] >= p.E) id[i] = -1;
+      any = any || id[i] >= 0;
+      sum += id[i] >= 0 ? wdw[i] : 0.0f;
+    }
+    sum = lanes_sum<G>(sum);
+    any = lanes_max<G>(any ? 1.0f : 0.0f) > 0.0f;
+    float top = x[0];
+#pragma unroll
+    for (int i = 1; i < VPL; ++i) top = fmaxf(top, x[i]);
+    top = lanes_max<G>(fmaxf(top, -INFINITY));
+    float e = 0.0f;
+#pragma unroll
+    for (int i = 0; i < VPL; ++i) e += x[i] = __expf(x[i] - top);
+    const float c = -__fdividef(sum, lanes_sum<G>(e)), m = sum / p.scale;
+#pragma unroll
+    for (int v = 0; v < VPL; v += W) {
+      const int at = expert_of<G, W>(v, sub);
+      if (VEC) {
+        typename Row<T, W>::type raw;
+        T* out = reinterpret_cast<T*>(&raw);
+#pragma unroll
+        for (int i = 0; i < W; ++i) out[i] = from_f32<T>(any ? x[v + i] * c : 0.0f);
+        if (mine && at < p.E) *reinterpret_cast<typename Row<T, W>::type*>(grad + at) = raw;
+      } else {
+#pragma unroll
+        for (int i = 0; i < W; ++i)
+          if (mine && at + i < p.E) grad[at + i] = from_f32<T>(any ? x[v + i] * c : 0.0f);
+      }
+    }
+    __syncwarp();   // the chosen places are written after the row
+#pragma unroll
+    for (int i = 0; i < kOuts; ++i) {
+      if (i * G >= k) break;
+      if (id[i] >= 0 && mine) grad[id[i]] = from_f32<T>(wdw[i] - w[i] * m);   // p_j = w_j / scale
     }
   }
 }
@@ -335,57 +529,88 @@ unsigned router_blocks(long long tokens, int sms, int threads_per_token, int blo
   return (unsigned)std::min(wanted, (long long)sms * blocks_per_sm);
 }
 
-template <typename T, int VPL>
+template <typename T, int G, int VPL>
 cudaError_t launch_forward_rows(const RouterParams& p, int sms, cudaStream_t stream) {
   constexpr int W = kVecOf<T, VPL>;
-  const unsigned blocks = router_blocks(p.tokens, sms, 32, 2048 / kRouterThreads);
-  if (p.E % W == 0 && aligned_to(p.logits, W * sizeof(T)) && (p.tokens == 1 || p.stride % W == 0))
-    router_forward_kernel<T, VPL, true><<<blocks, kRouterThreads, 0, stream>>>(p);
+  const unsigned blocks = router_blocks(p.tokens, sms, G, kRouterBlocksPerSm);
+  if (p.E % W == 0 && aligned_to(p.logits, W * sizeof(T)) && aligned_to(p.bias, 16) &&
+      (p.tokens == 1 || p.stride % W == 0))
+    p.bias ? router_forward_kernel<T, G, VPL, true, true><<<blocks, kRouterThreads, 0, stream>>>(p)
+           : router_forward_kernel<T, G, VPL, true, false><<<blocks, kRouterThreads, 0, stream>>>(p);
   else
-    router_forward_kernel<T, VPL, false><<<blocks, kRouterThreads, 0, stream>>>(p);
+    p.bias ? router_forward_kernel<T, G, VPL, false, true><<<blocks, kRouterThreads, 0, stream>>>(p)
+           : router_forward_kernel<T, G, VPL, false, false><<<blocks, kRouterThreads, 0, stream>>>(p);
   return cudaGetLastError();
 }
 
 template <typename T, bool SIGMOID, bool NORM>
 cudaError_t launch_forward(const RouterParams& p, int sms, cudaStream_t stream) {
-  if (p.E <= 32) return launch_forward_rows<T, 1>(p, sms, stream);
-  if (p.E <= 64) return launch_forward_rows<T, 2>(p, sms, stream);
-  if (p.E <= 128) return launch_forward_rows<T, 4>(p, sms, stream);
-  if (p.E <= 256) return launch_forward_rows<T, 8>(p, sms, stream);
-  if (p.E <= 512) return launch_forward_rows<T, 16>(p, sms, stream);
+  const bool few = p.tokens <= kFew * sms;
+  if (p.E <= 32) return launch_forward_rows<T, 8, 4>(p, sms, stream);
+  if (p.E <= 64) return launch_forward_rows<T, 8, 8>(p, sms, stream);
+  if (few && p.E <= 256) return launch_forward_rows<T, 32, 8>(p, sms, stream);
+  if (few && p.E <= 512) return launch_forward_rows<T, 32, 16>(p, sms, stream);
+  if (p.E <= 128) return launch_forward_rows<T, 8, 16>(p, sms, stream);
+  if (p.E <= 256) return launch_forward_rows<T, 8, 32>(p, sms, stream);
+  if (p.E <= 512) return launch_forward_rows<T, 16, 32>(p, sms, stream);
+  if (p.E <= 1024) return launch_forward_rows<T, 32, 32>(p, sms, stream);
   const long long blocks = (p.tokens + kRouterThreads / 32 - 1) / (kRouterThreads / 32);
   router_forward_any_kernel<T, SIGMOID, NORM><<<(unsigned)blocks, kRouterThreads, 0, stream>>>(p);
   return cudaGetLastError();
 }
 
-template <typename T, bool SIGMOID, bool NORM>
-cudaError_t launch_backward(const RouterParams& p, int, cudaStream_t stream) {
-  const long long blocks = (p.tokens + kRouterThreads / 32 - 1) / (kRouterThreads / 32);
-  router_backward_any_kernel<T, SIGMOID, NORM><<<(unsigned)blocks, kRouterThreads, 0, stream>>>(p);
+template <typename T, int G, int VPL>
+cudaError_t launch_backward_rows(const RouterParams& p, int sms, cudaStream_t stream) {
+  constexpr int W = kVecOf<T, VPL>;
+  const unsigned blocks = router_blocks(p.tokens, sms, G, kBackwardBlocksPerSm);
+  if (p.E % W == 0 && aligned_to(p.logits, W * sizeof(T)) && aligned_to(p.grad, W * sizeof(T)) &&
+      (p.tokens == 1 || (p.stride % W == 0 && p.grad_stride % W == 0)))
+    router_backward_all_kernel<T, G, VPL, true><<<blocks, kRouterThreads, 0, stream>>>(p);
+  else
+    router_backward_all_kernel<T, G, VPL, false><<<blocks, kRouterThreads, 0, stream>>>(p);
   return cudaGetLastError();
 }
 
 template <typename T>
-cudaError_t launch_typed(const RouterParams& p, bool sigmoid, bool norm, bool forward, int sms, cudaStream_t s) {
-  if (forward)
-    return sigmoid ? (norm ? launch_forward<T, true, true>(p, sms, s) : launch_forward<T, true, false>(p, sms, s))
-                   : (norm ? launch_forward<T, false, true>(p, sms, s) : launch_forward<T, false, false>(p, sms, s));
-  return sigmoid ? (norm ? launch_backward<T, true, true>(p, sms, s) : launch_backward<T, true, false>(p, sms, s))
-                 : (norm ? launch_backward<T, false, true>(p, sms, s) : launch_backward<T, false, false>(p, sms, s));
+cudaError_t launch_backward(const RouterParams& p, int sms, cudaStream_t stream) {
+  if (p.sigmoid || p.norm) {
+    constexpr int W = 16 / (int)sizeof(T);
+    const unsigned blocks = router_blocks(p.tokens, sms, 8, kSparseBlocksPerSm);
+    if (p.E % W == 0 && aligned_to(p.grad, 16) && (p.tokens == 1 || p.grad_stride % W == 0))
+      router_backward_sparse_kernel<T, true><<<blocks, kRouterThreads, 0, stream>>>(p);
+    else
+      router_backward_sparse_kernel<T, false><<<blocks, kRouterThreads, 0, stream>>>(p);
+    return cudaGetLastError();
+  }
+  if (p.E <= 32) return launch_backward_rows<T, 8, 4>(p, sms, stream);
+  if (p.E <= 64) return launch_backward_rows<T, 8, 8>(p, sms, stream);
+  if (p.E <= 128) return launch_backward_rows<T, 16, 8>(p, sms, stream);
+  if (p.E <= 256) return launch_backward_rows<T, 32, 8>(p, sms, stream);
+  if (p.E <= 512) return launch_backward_rows<T, 32, 16>(p, sms, stream);
+  if (p.E <= 1024) return launch_backward_rows<T, 32, 32>(p, sms, stream);
+  const long long blocks = (p.tokens + kRouterThreads / 32 - 1) / (kRouterThreads / 32);
+  router_backward_any_kernel<T><<<(unsigned)blocks, kRouterThreads, 0, stream>>>(p);
+  return cudaGetLastError();
+}
+
+template <typename T>
+cudaError_t launch_typed(const RouterParams& p, bool forward, int sms, cudaStream_t s) {
+  if (!forward) return launch_backward<T>(p, sms, s);
+  return p.sigmoid ? (p.norm ? launch_forward<T, true, true>(p, sms, s) : launch_forward<T, true, false>(p, sms, s))
+                   : (p.norm ? launch_forward<T, false, true>(p, sms, s) : launch_forward<T, false, false>(p, sms, s));
 }
 
 int launch(const topoep_router_config* cfg, RouterParams& p, bool forward, cudaStream_t s) {
-  const bool sigmoid = cfg->score == TOPOEP_SCORE_SIGMOID, norm = cfg->normalize != 0;
-  p.sigmoid = sigmoid;
-  p.norm = norm;
+  p.sigmoid = cfg->score == TOPOEP_SCORE_SIGMOID;
+  p.norm = cfg->normalize != 0;
   int dev = 0, sms = 0;
   cudaError_t e = cudaGetDevice(&dev);
   if (e == cudaSuccess) e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
   if (e != cudaSuccess) return TOPOEP_ERR_CUDA;
   switch (cfg->dtype) {
-    case TOPOEP_DTYPE_F32: e = launch_typed<float>(p, sigmoid, norm, forward, sms, s); break;
-    case TOPOEP_DTYPE_BF16: e = launch_typed<__nv_bfloat16>(p, sigmoid, norm, forward, sms, s); break;
-    default: e = launch_typed<__half>(p, sigmoid, norm, forward, sms, s); break;
+    case TOPOEP_DTYPE_F32: e = launch_typed<float>(p, forward, sms, s); break;
+    case TOPOEP_DTYPE_BF16: e = launch_typed<__nv_bfloat16>(p, forward, sms, s); break;
+    default: e = launch_typed<__half>(p, forward, sms, s); break;
   }
   return e == cudaSuccess ? TOPOEP_OK : TOPOEP_ERR_CUDA;
 }

@@ -1,6 +1,7 @@
 // Router of an MoE layer: scores of a token's experts -> ids and weights of the chosen ones, and
 // the gradient of the scores.  The definitions stand in topoep.h.
 #include <algorithm>
+#include <atomic>
 #include <cfloat>
 #include <climits>
 #include <cmath>
@@ -605,7 +606,14 @@ int launch(const topoep_router_config* cfg, RouterParams& p, bool forward, cudaS
   p.norm = cfg->normalize != 0;
   int dev = 0, sms = 0;
   cudaError_t e = cudaGetDevice(&dev);
-  if (e == cudaSuccess) e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
+  // the attribute is asked for once a device; two threads would store the same number
+  static std::atomic<int> known[64];
+  const bool kept = e == cudaSuccess && dev >= 0 && dev < 64;
+  if (kept) sms = known[dev].load(std::memory_order_relaxed);
+  if (e == cudaSuccess && sms == 0) {
+    e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
+    if (e == cudaSuccess && kept) known[dev].store(sms, std::memory_order_relaxed);
+  }
   if (e != cudaSuccess) return TOPOEP_ERR_CUDA;
   switch (cfg->dtype) {
     case TOPOEP_DTYPE_F32: e = launch_typed<float>(p, forward, sms, s); break;

@@ -24,34 +24,37 @@ def _raise(rc: int):
         raise B.TopoEPError(rc)
 
 
-class _On:
-    """The stream and device a call runs on: the caller's stream, or the current one of the
-    device.  Tensors the call allocates belong to that stream, and tensors it is given are marked
-    as used there, so that their memory is not handed out again before the call is done."""
+# address of a device's current stream without the Stream object around it
+_current_raw = getattr(torch._C, "_cuda_getCurrentRawStream", None) or \
+    (lambda index: torch.cuda.current_stream(index).cuda_stream)
 
-    def __init__(self, device: torch.device, stream: Optional[torch.cuda.Stream], given=()):
-        self.device = device
-        self.index = device.index
-        current = torch.cuda.current_stream(device)
-        self.raw = current.cuda_stream if stream is None else stream.cuda_stream
-        self.guard = None
-        if stream is not None and stream.cuda_stream != current.cuda_stream:
-            _check(stream.device_index == self.index, "the stream belongs to another device")
+
+class _Elsewhere:
+    """A call on a stream of the caller's choice, or on a device that is not the current one.
+    Tensors the call allocates belong to that stream, and tensors it is given are marked as used
+    there, so that their memory is not handed out again before the call is done."""
+
+    def __init__(self, index: int, stream: Optional[torch.cuda.Stream], given):
+        if stream is None:
+            self.guard = torch.cuda.device(index)
+        else:
+            _check(stream.device_index == index, "the stream belongs to another device")
             self.guard = torch.cuda.stream(stream)
             for t in given:
                 if t is not None:
                     t.record_stream(stream)
-        elif torch.cuda.current_device() != self.index:
-            self.guard = torch.cuda.device(self.index)
 
     def __enter__(self):
-        if self.guard is not None:
-            self.guard.__enter__()
-        return self.raw
+        self.guard.__enter__()
 
     def __exit__(self, *exc):
-        if self.guard is not None:
-            self.guard.__exit__(*exc)
+        self.guard.__exit__(*exc)
+
+
+def _at_home(index: int, stream: Optional[torch.cuda.Stream]) -> bool:
+    """The call runs on the current stream of the current device: nothing to set up."""
+    return torch.cuda.current_device() == index and \
+        (stream is None or stream.cuda_stream == _current_raw(index))
 
 
 def _workspace(nbytes: int, device: torch.device):
@@ -95,18 +98,18 @@ class Router:
         _raise(B.topoep_router_forward(self._cfg[torch.float32], None, self.experts, 0, None, None,
                                        None, None))
 
-    def _rows(self, t: torch.Tensor, what: str) -> torch.Tensor:
+    def _rows(self, t: torch.Tensor, what: str):
+        """(rows, tokens, elements between rows) of [...][experts]."""
+        E = self.experts
         _check(t.is_cuda and t.dtype in _DTYPES, what + ": a float32, bfloat16 or float16 CUDA tensor")
-        _check(t.dim() >= 1 and t.shape[-1] == self.experts,
-               "%s: the last dimension has %d experts" % (what, self.experts))
-        if t.dim() != 2:
-            t = t.reshape(-1, self.experts)
-        _check(t.shape[1] <= 1 or t.stride(1) == 1, what + ": experts of a token are adjacent")
-        _check(t.shape[0] <= 1 or t.stride(0) >= self.experts, what + ": rows do not overlap")
-        return t
-
-    def _stride(self, t: torch.Tensor) -> int:
-        return t.stride(0) if t.shape[0] > 1 else self.experts
+        shape = t.shape
+        _check(len(shape) >= 1 and shape[-1] == E, "%s: the last dimension has %d experts" % (what, E))
+        if len(shape) != 2:
+            t = t.reshape(-1, E)
+        T, (between, within) = t.shape[0], t.stride()
+        _check(E == 1 or within == 1, what + ": experts of a token are adjacent")
+        _check(T <= 1 or between >= E, what + ": rows do not overlap")
+        return t, T, between if T > 1 else E
 
     def forward(self, logits: torch.Tensor, bias: Optional[torch.Tensor] = None,
                 mask: Optional[torch.Tensor] = None, stream=None):
@@ -114,40 +117,49 @@ class Router:
 
         bias [experts] float32 is added to the sigmoid scores for the choice alone; mask [...]
         (bool or uint8) leaves out the tokens where it is 0: ids -1, weights 0."""
-        rows = self._rows(logits, "logits")
-        T, lead = rows.shape[0], logits.shape[:-1]
+        rows, T, stride = self._rows(logits, "logits")
+        index = rows.get_device()
         if bias is not None:
             _check(bias.dtype == torch.float32 and bias.is_contiguous() and
-                   bias.device == rows.device and tuple(bias.shape) == (self.experts,),
+                   bias.get_device() == index and bias.shape == (self.experts,),
                    "bias: [experts] float32, contiguous, on the logits' device")
         if mask is not None:
             _check(mask.dtype in (torch.bool, torch.uint8) and mask.is_contiguous() and
-                   mask.device == rows.device and mask.shape == lead,
+                   mask.get_device() == index and mask.shape == logits.shape[:-1],
                    "mask: bool or uint8, contiguous, one value a token, on the logits' device")
-        with _On(rows.device, stream, (logits, bias, mask)) as raw:
-            ids = torch.empty(lead + (self.top_k,), dtype=torch.int32, device=rows.device)
-            weights = torch.empty(lead + (self.top_k,), dtype=torch.float32, device=rows.device)
-            _raise(B.topoep_router_forward(self._cfg[rows.dtype], rows, self._stride(rows), T, bias,
-                                           mask, ids, weights, raw))
+        if not _at_home(index, stream):
+            with _Elsewhere(index, stream, (logits, bias, mask)):
+                return self.forward(logits, bias, mask)
+        want = logits.shape[:-1] + (self.top_k,)
+        ids = rows.new_empty(want, dtype=torch.int32)
+        weights = rows.new_empty(want, dtype=torch.float32)
+        _raise(B.topoep_router_forward(self._cfg[rows.dtype], rows.data_ptr(), stride, T,
+                                       bias.data_ptr() if bias is not None else None,
+                                       mask.data_ptr() if mask is not None else None,
+                                       ids.data_ptr(), weights.data_ptr(), _current_raw(index)))
         return ids, weights
 
     def backward(self, logits: torch.Tensor, ids: torch.Tensor, weights: torch.Tensor,
                  grad_weights: torch.Tensor, stream=None) -> torch.Tensor:
         """Gradient of the logits (their type and shape) from the gradient of the weights."""
-        rows = self._rows(logits, "logits")
-        T, want = rows.shape[0], logits.shape[:-1] + (self.top_k,)
+        rows, T, stride = self._rows(logits, "logits")
+        index, want = rows.get_device(), logits.shape[:-1] + (self.top_k,)
         _check(ids.dtype == torch.int32 and ids.is_contiguous() and ids.shape == want and
-               ids.device == rows.device, "ids: as forward() returned them")
+               ids.get_device() == index, "ids: as forward() returned them")
         _check(weights.dtype == torch.float32 and weights.is_contiguous() and
-               weights.shape == want and weights.device == rows.device,
+               weights.shape == want and weights.get_device() == index,
                "weights: as forward() returned them")
         _check(grad_weights.dtype == torch.float32 and grad_weights.shape == want and
-               grad_weights.device == rows.device, "grad_weights: float32, shaped as the weights")
-        with _On(rows.device, stream, (logits, ids, weights, grad_weights)) as raw:
-            grad_weights = grad_weights.contiguous()
-            grad = torch.empty(logits.shape, dtype=rows.dtype, device=rows.device)
-            _raise(B.topoep_router_backward(self._cfg[rows.dtype], rows, self._stride(rows), T, ids,
-                                            weights, grad_weights, grad, self.experts, raw))
+               grad_weights.get_device() == index, "grad_weights: float32, shaped as the weights")
+        if not _at_home(index, stream):
+            with _Elsewhere(index, stream, (logits, ids, weights, grad_weights)):
+                return self.backward(logits, ids, weights, grad_weights)
+        grad_weights = grad_weights.contiguous()
+        grad = rows.new_empty(logits.shape)
+        _raise(B.topoep_router_backward(self._cfg[rows.dtype], rows.data_ptr(), stride, T,
+                                        ids.data_ptr(), weights.data_ptr(),
+                                        grad_weights.data_ptr(), grad.data_ptr(), self.experts,
+                                        _current_raw(index)))
         return grad
 
     def __call__(self, logits: torch.Tensor, bias: Optional[torch.Tensor] = None,
@@ -174,6 +186,7 @@ class TokenExperts:
         self.device = torch.device(device) if device is not None else torch.device("cuda")
         if self.device.index is None:
             self.device = torch.device("cuda", torch.cuda.current_device())
+        self._index = self.device.index
         self._params = None
         nbytes = B.topoep_experts_workspace_bytes(handle)
         with torch.cuda.device(self.device):
@@ -217,30 +230,34 @@ class TokenExperts:
         """y [tokens][hidden] bfloat16 of x [tokens][hidden] bfloat16, instance ids [tokens][top_k]
         int32 (the plan's token_replica rows) and weights [tokens][top_k] float32."""
         _check(x.dim() == 2 and x.dtype == torch.bfloat16 and x.shape[1] == self.hidden and
-               x.device == self.device, "x: [tokens][hidden] bfloat16 on this device")
-        T = x.shape[0]
+               x.get_device() == self._index, "x: [tokens][hidden] bfloat16 on this device")
+        T, (between, within) = x.shape[0], x.stride()
         _check(T <= self.max_tokens, "at most %d tokens" % self.max_tokens)
-        _check(x.shape[1] == 1 or x.stride(1) == 1, "x: elements of a row are adjacent")
-        _check(T <= 1 or x.stride(0) >= self.hidden or x.stride(0) == 0, "x: rows do not overlap")
-        if T > 1 and x.stride(0) == 0:   # one row for every token
-            x = x.contiguous()
+        _check(self.hidden == 1 or within == 1, "x: elements of a row are adjacent")
+        _check(T <= 1 or between >= self.hidden or between == 0, "x: rows do not overlap")
         want = (T, self.top_k)
-        _check(ids.dtype == torch.int32 and ids.is_contiguous() and tuple(ids.shape) == want and
-               ids.device == self.device, "ids: [tokens][top_k] int32, contiguous, on this device")
+        _check(ids.dtype == torch.int32 and ids.is_contiguous() and ids.shape == want and
+               ids.get_device() == self._index,
+               "ids: [tokens][top_k] int32, contiguous, on this device")
         _check(weights.dtype == torch.float32 and weights.is_contiguous() and
-               tuple(weights.shape) == want and weights.device == self.device,
+               weights.shape == want and weights.get_device() == self._index,
                "weights: [tokens][top_k] float32, contiguous, on this device")
-        with _On(self.device, stream, (x, ids, weights, out)) as raw:
-            if out is None:
-                out = torch.empty((T, self.hidden), dtype=torch.bfloat16, device=self.device)
-            else:
-                _check(out.dtype == torch.bfloat16 and tuple(out.shape) == (T, self.hidden) and
-                       out.device == self.device and (self.hidden == 1 or out.stride(1) == 1) and
-                       (T <= 1 or out.stride(0) >= self.hidden),
-                       "out: [tokens][hidden] bfloat16 on this device, elements of a row adjacent")
-            _raise(B.topoep_experts_forward(self.handle, x, x.stride(0) if T > 1 else self.hidden,
-                                            ids, weights, T, out,
-                                            out.stride(0) if T > 1 else self.hidden, raw))
+        if out is not None:
+            _check(out.dtype == torch.bfloat16 and out.shape == (T, self.hidden) and
+                   out.get_device() == self._index and (self.hidden == 1 or out.stride(1) == 1) and
+                   (T <= 1 or out.stride(0) >= self.hidden),
+                   "out: [tokens][hidden] bfloat16 on this device, elements of a row adjacent")
+        if not _at_home(self._index, stream):
+            with _Elsewhere(self._index, stream, (x, ids, weights, out)):
+                return self.forward(x, ids, weights, out)
+        if T > 1 and between == 0:   # one row for every token
+            x, between = x.contiguous(), self.hidden
+        if out is None:
+            out = x.new_empty((T, self.hidden))
+        _raise(B.topoep_experts_forward(self.handle, x.data_ptr(), between if T > 1 else self.hidden,
+                                        ids.data_ptr(), weights.data_ptr(), T, out.data_ptr(),
+                                        out.stride(0) if T > 1 else self.hidden,
+                                        _current_raw(self._index)))
         return out
 
     __call__ = forward
@@ -341,11 +358,13 @@ class GradientClip:
         return self._call(float(max_norm), stream)
 
     def _call(self, max_norm, stream):
-        given = () if stream is None else [t for both in self._tensors for t in both]
-        with _On(self.device, stream, given) as raw:
-            value = torch.empty((), dtype=torch.float32, device=self.device)
-            if max_norm is None:
-                _raise(B.topoep_clip_norm(self.handle, self._kind, value, raw))
-            else:
-                _raise(B.topoep_clip_run(self.handle, self._kind, max_norm, value, raw))
+        index = self.device.index
+        if not _at_home(index, stream):
+            with _Elsewhere(index, stream, [t for both in self._tensors for t in both]):
+                return self._call(max_norm, None)
+        value = torch.empty((), dtype=torch.float32, device=self.device)
+        if max_norm is None:
+            _raise(B.topoep_clip_norm(self.handle, self._kind, value, _current_raw(index)))
+        else:
+            _raise(B.topoep_clip_run(self.handle, self._kind, max_norm, value, _current_raw(index)))
         return value

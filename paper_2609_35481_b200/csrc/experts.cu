@@ -782,6 +782,154 @@ experts_kernel(const __grid_constant__ Maps maps, const __grid_constant__ LayerP
   }
 }
 
+// --------------------------------------------------------------------- the kernel of one token
+//
+// Latency counts, and a weight meets one value, so ordinary multiply-adds keep up with the memory
+// (about 40 instructions a KB: a quarter of the issue slots).  A warp takes whole rows of weights, so
+// no sum is cut between CTAs:
+//   1. the token's row goes to shared memory in 32 bits; a warp reads row f of gate and up of an
+//      instance and writes h[id][f] in 32 bits;
+//   2. all CTAs wait for one another once, the first of their rows of the down matrix being
+//      fetched into L2 meanwhile;
+//   3. a CTA owns hidden / CTAs outputs: its warps take (output, id) rows of the down matrix, and
+//      the sums, weighed, are added up in the order of the ids.
+// Against the tensor-core kernel with one token: two experts of 1024 x 2048 (25 MB) 11.7 against
+// 19.9 us, eight of 7168 x 2048 (705 MB) 110 against 121 us (6.4 TB/s); with two tokens that kernel
+// is at the speed of the memory itself (1.06 GB in 166 us).  24 warps: with 16 it is 114 us, with 32
+// (and half the loads in flight for each) 113 us and 10.2 us for the small one.
+constexpr int kOneThreads = 768, kOneWarps = kOneThreads / 32, kMaxIds = 16;
+constexpr int kOneAhead = 128 * 1024;        // bytes of a CTA's down rows fetched before the wait
+constexpr size_t kOneShared = 160 * 1024;    // most bytes of the token's row or a CTA's sums
+
+__device__ __forceinline__ void unpack8(const uint4& v, float (&f)[8]) {
+  const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    f[2 * i] = __uint_as_float(w[i] << 16);
+    f[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+  }
+}
+
+// Sums of n weights at `w` (and at `w2` if TWO) times n values at v; the same in every lane.
+template <bool TWO>
+__device__ __forceinline__ float2 dot_row(const __nv_bfloat16* w, const __nv_bfloat16* w2, int n, const float* v, int lane) {
+  constexpr int kAhead = TWO ? 4 : 8;   // 16 bytes a lane each
+  const int vecs = n >> 3;
+  float sum = 0.0f, sum2 = 0.0f;
+  for (int base = lane; base < vecs; base += 32 * kAhead) {
+    uint4 a[kAhead], b[kAhead];
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) {
+      const int q = base + 32 * i;
+      if (q < vecs) {
+        a[i] = __ldcs(reinterpret_cast<const uint4*>(w) + q);
+        if (TWO) b[i] = __ldcs(reinterpret_cast<const uint4*>(w2) + q);
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) {
+      const int q = base + 32 * i;
+      if (q >= vecs) break;
+      float fa[8], fb[8];
+      unpack8(a[i], fa);
+      if (TWO) unpack8(b[i], fb);
+      const float4* x = reinterpret_cast<const float4*>(v) + 2 * q;
+      const float4 x0 = x[0], x1 = x[1];
+      const float xs[8] = {x0.x, x0.y, x0.z, x0.w, x1.x, x1.y, x1.z, x1.w};
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        sum = fmaf(fa[e], xs[e], sum);
+        if (TWO) sum2 = fmaf(fb[e], xs[e], sum2);
+      }
+    }
+  }
+  return make_float2(warp_sum(sum), TWO ? warp_sum(sum2) : 0.0f);
+}
+
+struct OneParams {
+  ExpertsParams e;
+  uint32_t* control;
+};
+
+__global__ void __launch_bounds__(kOneThreads, 1) experts_one_kernel(const __grid_constant__ OneParams p) {
+  extern __shared__ __align__(16) float room[];   // the token's row, then sums [output][id]
+  __shared__ const __nv_bfloat16* block[kMaxIds];
+  __shared__ float weight[kMaxIds];
+  __shared__ int n_shared, failed;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, cta = blockIdx.x, G = gridDim.x;
+  const int H = p.e.H, F = p.e.F;
+  if (warp == 0) {   // the valid ids, in their order
+    const int id = lane < p.e.k ? p.e.ids[lane] : -1;
+    const float w = lane < p.e.k ? p.e.weights[lane] : 0.0f;
+    const bool good = id >= 0 && id < p.e.instances;
+    if (!good && id != -1 && cta == 0) atomicOr(p.control + C_STATUS, TOPOEP_FLAG_BAD_ID);
+    const unsigned all = __ballot_sync(0xffffffffu, good);
+    if (good) {
+      const int at = __popc(all & ((1u << lane) - 1));
+      block[at] = block_of(p.e, id);
+      weight[at] = w;
+    }
+    if (lane == 0) { n_shared = __popc(all); failed = 0; }
+  } else {
+    for (int q = tid - 32; q < H / 8; q += kOneThreads - 32) {
+      float f[8];
+      unpack8(*(reinterpret_cast<const uint4*>(p.e.x) + q), f);
+      float4* to = reinterpret_cast<float4*>(room) + 2 * q;
+      to[0] = make_float4(f[0], f[1], f[2], f[3]);
+      to[1] = make_float4(f[4], f[5], f[6], f[7]);
+    }
+  }
+  __syncthreads();
+  const int n = n_shared;
+
+  // ---- gate and up
+  for (int u = warp * G + cta; u < n * F; u += kOneWarps * G) {
+    const int s = u / F, f = u - s * F;
+    const __nv_bfloat16* wg = block[s] + (long long)f * H;
+    const float2 gu = dot_row<true>(wg, wg + (long long)F * H, H, room, lane);
+    if (lane == 0) p.e.h[u] = gu.x / (1.0f + expf(-gu.x)) * gu.y;
+  }
+  const int c0 = (int)((long long)H * cta / G), c1 = (int)((long long)H * (cta + 1) / G);
+  const int units = (c1 - c0) * n;
+  {   // the first down rows, a 128-byte line a thread
+    const int lines = (F * 2 + 127) / 128, ahead = min(units, kOneAhead / (F * 2));
+    for (int i = tid; i < ahead * lines; i += kOneThreads) {
+      const int unit = i / lines, c = unit / n, s = unit - c * n;
+      const char* row = reinterpret_cast<const char*>(block[s] + 2ll * F * H + (long long)(c0 + c) * F);
+      const int at = min((i - unit * lines) * 128, 2 * F - 16);   // inside the row
+      asm volatile("prefetch.global.L2 [%0];" ::"l"(row + at));
+    }
+  }
+  __threadfence();
+  __syncthreads();
+  if (tid == 0) {
+    add_release(p.control + C_ARRIVE, 1);
+    if (!spin_until(p.control + C_ARRIVE, G)) failed = 1;
+  }
+  __syncthreads();
+
+  // ---- down
+  for (int unit = warp; unit < units; unit += kOneWarps) {
+    const int c = unit / n, s = unit - c * n;
+    const __nv_bfloat16* wd = block[s] + 2ll * F * H + (long long)(c0 + c) * F;
+    const float2 v = dot_row<false>(wd, wd, F, p.e.h + (long long)s * F, lane);
+    if (lane == 0) room[unit] = v.x;   // the token's row is done with
+  }
+  __syncthreads();
+  for (int c = tid; c < c1 - c0; c += kOneThreads) {
+    float y = 0.0f;
+    for (int s = 0; s < n; ++s) y += weight[s] * room[c * n + s];
+    p.e.y[c0 + c] = __float2bfloat16_rn(y);
+  }
+  if (tid == 0) {
+    if (failed) atomicOr(p.control + C_STATUS, TOPOEP_FLAG_INTERNAL);
+    if (atomicAdd(p.control + C_LEAVE, 1) + 1 == (unsigned)G) {   // ready for the next call
+      p.control[C_ARRIVE] = 0;
+      p.control[C_LEAVE] = 0;
+    }
+  }
+}
+
 constexpr size_t kAlign = 256;
 inline size_t align_up(size_t x) { return (x + kAlign - 1) / kAlign * kAlign; }
 
@@ -911,6 +1059,8 @@ extern "C" int topoep_experts_set_workspace(topoep_experts_t h, void* dev_ptr, s
     if (e == cudaSuccess) e = cudaMemset(ws + h->off_partial, 0, h->off_yp - h->off_partial);   // no tags
     if (e == cudaSuccess)
       e = cudaFuncSetAttribute(experts_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSharedLimit);
+    if (e == cudaSuccess)
+      e = cudaFuncSetAttribute(experts_one_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kOneShared);
     if (e != cudaSuccess) return TOPOEP_ERR_CUDA;
     h->encode = encode_fn();
     if (!h->encode || !encode(h->encode, &h->maps.h, ws + h->off_h, 2, h->ffn, 2 * h->max_rows, 1,
@@ -997,6 +1147,32 @@ cudaError_t launch_tiled(topoep_experts_t h, const ExpertsParams& a, cudaStream_
 
 }  // namespace
 
+namespace {
+
+// Shared memory of the kernel of one token: its row, or the sums of a CTA's outputs.
+size_t one_shared(const ExpertsParams& a, int ctas) {
+  return std::max((size_t)a.H, (size_t)(a.H / ctas + 1) * a.k) * sizeof(float);
+}
+
+cudaError_t launch_one(topoep_experts_t h, const ExpertsParams& a, cudaStream_t stream) {
+  OneParams p = {};
+  p.e = a;
+  p.control = reinterpret_cast<uint32_t*>(h->ws);
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(h->ctas);
+  cfg.blockDim = dim3(kOneThreads);
+  cfg.dynamicSmemBytes = one_shared(a, h->ctas);
+  cfg.stream = stream;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeCooperative;
+  attr[0].val.cooperative = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, experts_one_kernel, p);
+}
+
+}  // namespace
+
 extern "C" int topoep_experts_forward(topoep_experts_t h, const void* dev_x, int64_t x_row_stride,
                                       const int32_t* dev_ids, const float* dev_weights, int tokens,
                                       void* dev_y, int64_t y_row_stride, topoep_stream_t stream) {
@@ -1031,7 +1207,8 @@ extern "C" int topoep_experts_forward(topoep_experts_t h, const void* dev_x, int
   p.instances = h->instances;
   cudaError_t e;
   if (h->tiled && aligned_to(dev_x, 16) && (tokens == 1 || x_row_stride % 8 == 0)) {
-    e = launch_tiled(h, p, st);
+    const bool one = tokens == 1 && one_shared(p, h->ctas) <= kOneShared;
+    e = one ? launch_one(h, p, st) : launch_tiled(h, p, st);
   } else {
     const int per = kAnyThreads / 32;
     experts_gate_any_kernel<<<dim3((p.F + per - 1) / per, tokens * p.k), kAnyThreads, 0, st>>>(p);

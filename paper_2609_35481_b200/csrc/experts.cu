@@ -23,8 +23,8 @@
 // Between 1 and 2 only the copies of h wait, each for its instance's tiles: the copies of the
 // weights, issued by another warp, run ahead and keep the memory busy meanwhile.
 //
-// Roles of a CTA's eight warps: 0 copies weights, 1 copies token rows, 2 issues the products, 4-7
-// read the accumulators (double-buffered in tensor memory).  The launch is cooperative: every CTA
+// Roles of a CTA's warps: 0 copies weights, 1 copies token rows, 2 issues the products, 4-7 read the
+// accumulators (double-buffered in tensor memory); all sixteen take part in 0 and 3.  The launch is cooperative: every CTA
 // is resident, so the waits of 2 and 3 end; all waits are bounded all the same and set
 // TOPOEP_FLAG_INTERNAL when they run out.
 #include <cuda.h>
@@ -107,15 +107,15 @@ __global__ void __launch_bounds__(kAnyThreads) experts_down_any_kernel(const Exp
 
 // ------------------------------------------------------------------- the tensor-core kernel
 
-constexpr int kThreads = 256;
+constexpr int kThreads = 512;
 constexpr int kTileM = 128;             // rows of one product; a stage holds two
 constexpr int kStepK = 64;              // elements of the sum in a step: one 128-byte swizzled row
 constexpr int kHalfBytes = kTileM * kStepK * 2;
 constexpr int kStageA = 2 * kHalfBytes;
 constexpr int kIdsPerThread = 128 * 16 / kThreads;   // most tokens x most ids a token
 constexpr int kMaxStages = 8;
-constexpr unsigned kWaitLimit = 1u << 25;   // polls of a wait (about a second) before it is given up
-constexpr unsigned kSpinLimit = 1u << 22;   // polls of a word in global memory (a few seconds)
+constexpr unsigned kWaitLimit = 1u << 24;   // polls of a wait (some 0.2 s) before it is given up
+constexpr unsigned kSpinLimit = 1u << 20;   // polls of a word in global memory (about a second)
 
 // Words of the workspace's control block.  The counters are zero between calls; the serial number
 // counts the calls and tags their parts of cut tiles.
@@ -565,7 +565,7 @@ experts_kernel(const __grid_constant__ Maps maps, const __grid_constant__ LayerP
       if (!ok) *failed = 1;
     }
     __syncwarp();
-  } else if (warp >= 4) {   // ---- accumulators
+  } else if (warp >= 4 && warp < 8) {   // ---- accumulators
     const int quad = warp & 3, row = quad * 32 + lane, etid = tid - 128;
     int buf = 0;
     uint32_t accph = 0;
@@ -674,7 +674,7 @@ experts_kernel(const __grid_constant__ Maps maps, const __grid_constant__ LayerP
     // The 256 outputs of a token that a tile of rows gives are one item: lane j works out where the
     // parts of id j are, then all lanes read eight outputs of every part, eight parts at a time.  A
     // warp takes an item; when there are fewer items than CTAs, the warps of a CTA share one, each
-    // taking every eighth part (one token, eight ids: 4.5 us after the last partial result with a
+    // taking every sixteenth part (one token, eight ids: 4.5 us after the last partial result with a
     // warp an item, 2 us shared).
     constexpr int kWarps = kThreads / 32;
     const int items = p.tokens * per_slot2;

@@ -558,8 +558,9 @@ int topoep_experts_read_status(topoep_experts_t h, uint32_t* host_flags);
  *
  * A tensor is rows of cols elements, src_row_stride / dst_row_stride elements apart (>= cols when
  * rows > 1).  dst NULL or equal to src: in place (the strides have to agree).  Otherwise a dst
- * overlaps no tensor.  Tensors with rows or cols 0 are left out.  Pointers need only their
- * element's alignment.
+ * overlaps no tensor.  A gradient that is shared is listed once: outputs that are one run of
+ * elements and overlap, or begin at the same place, are refused (TOPOEP_ERR_ARG).  Tensors with
+ * rows or cols 0 are left out.  Pointers need only their element's alignment.
  *   topoep_clip_create        copies the list; count >= 0; host memory only
  *   topoep_clip_set_workspace as topoep_set_workspace: uploads the list, synchronises the device
  *   topoep_clip_norm          writes *dev_norm (float) only

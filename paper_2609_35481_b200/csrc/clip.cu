@@ -17,6 +17,7 @@
 // 64 bits beyond that; a sum of squares outside [2^-60, 2^126] (gradients so small or large that
 // squares leave the range, zeros, infinities, NaN) is formed again in 64 bits from the same
 // registers.
+#include <algorithm>
 #include <climits>
 #include <cmath>
 #include <new>
@@ -41,7 +42,7 @@ constexpr unsigned kSpinLimit = 1u << 22;   // polls of a word (a few seconds) b
 constexpr float kClipEps = 1e-6f;
 
 // Adjacent elements src[0 .. n) -> dst[0 .. n); with `tensor` >= 0, n elements of a tensor of short
-// rows beginning with element `first` of it.
+// rows, src and dst being the first row of the chunk and `first` its first element there.
 struct ClipChunk {
   const void* src;
   void* dst;
@@ -49,11 +50,12 @@ struct ClipChunk {
   int dtype;
   int tensor;
   int scalar;   // 1: source and output differ modulo 16 bytes
-  long long first;
+  int first, pad;
 };
 
 struct ClipRows {
-  long long cols, src_stride, dst_stride;
+  long long src_stride, dst_stride;
+  unsigned cols, pad;
 };
 
 struct ClipParams {
@@ -207,9 +209,10 @@ struct Body {
   }
 };
 
-// Element i of a tensor of short rows, in elements from its start.
-__device__ __forceinline__ long long offset_of(long long i, long long cols, long long stride) {
-  return i / cols * stride + i % cols;
+// Element i of a chunk of short rows (fewer than kMinChunkBytes elements each), in elements.
+__device__ __forceinline__ long long offset_of(const ClipRows& r, unsigned i, long long stride) {
+  const unsigned row = i / r.cols;
+  return row * stride + (i - row * r.cols);
 }
 
 template <int KIND>
@@ -220,7 +223,7 @@ __device__ __forceinline__ double norm_chunk(const ClipRows* rows, const ClipChu
   if (c.tensor >= 0) {
     const ClipRows r = rows[c.tensor];
     for (int i = lane; i < c.n; i += 32)
-      sum = join<KIND>(sum, take_one<KIND>(load_one(src + (offset_of(c.first + i, r.cols, r.src_stride) << b.shift), c.dtype)));
+      sum = join<KIND>(sum, take_one<KIND>(load_one(src + (offset_of(r, c.first + i, r.src_stride) << b.shift), c.dtype)));
     return sum;
   }
   if (lane < b.head) sum = take_one<KIND>(load_one(src + (lane << b.shift), c.dtype));
@@ -247,8 +250,8 @@ __device__ __forceinline__ void scale_chunk(const ClipRows* rows, const ClipChun
   if (c.tensor >= 0) {
     const ClipRows r = rows[c.tensor];
     for (int i = lane; i < c.n; i += 32)
-      store_one(dst + (offset_of(c.first + i, r.cols, r.dst_stride) << b.shift), c.dtype,
-                load_one(src + (offset_of(c.first + i, r.cols, r.src_stride) << b.shift), c.dtype) * factor);
+      store_one(dst + (offset_of(r, c.first + i, r.dst_stride) << b.shift), c.dtype,
+                load_one(src + (offset_of(r, c.first + i, r.src_stride) << b.shift), c.dtype) * factor);
     return;
   }
   if (c.scalar) {
@@ -393,6 +396,33 @@ static void cut_run(topoep_clip_ctx* h, const char* src, char* dst, long long n,
   }
 }
 
+// True if two outputs of one run of adjacent elements each overlap, or one is there twice: a shared
+// gradient would be scaled twice.
+static bool outputs_overlap(int64_t count, const topoep_grad_tensor* tensors) {
+  struct Run { uintptr_t begin, end; int64_t cols, stride; };
+  std::vector<Run> runs;
+  for (int64_t i = 0; i < count; ++i) {
+    const topoep_grad_tensor& g = tensors[i];
+    if (g.rows == 0 || g.cols == 0) continue;
+    const int64_t stride = g.rows == 1 ? g.cols : g.dst ? g.dst_row_stride : g.src_row_stride;
+    const uintptr_t begin = reinterpret_cast<uintptr_t>(g.dst ? g.dst : g.src);
+    const uintptr_t bytes = (uintptr_t)((g.rows - 1) * stride + g.cols) * dtype_bytes(g.dtype);
+    runs.push_back({begin, begin + bytes, g.cols, stride});
+  }
+  std::sort(runs.begin(), runs.end(), [](const Run& a, const Run& b) { return a.begin < b.begin; });
+  uintptr_t end = 0;   // of the runs so far
+  for (size_t i = 0; i < runs.size(); ++i) {
+    const Run& r = runs[i];
+    if (r.cols == r.stride) {
+      if (r.begin < end) return true;
+      end = r.end;
+    } else if (i > 0 && runs[i - 1].begin == r.begin) {
+      return true;
+    }
+  }
+  return false;
+}
+
 static int list_chunks(topoep_clip_ctx* h, int64_t count, const topoep_grad_tensor* tensors) {
   double total = 0.0;
   for (int64_t i = 0; i < count; ++i) {
@@ -409,6 +439,7 @@ static int list_chunks(topoep_clip_ctx* h, int64_t count, const topoep_grad_tens
     if (!aligned_to(g.src, dtype_bytes(g.dtype)) || !aligned_to(g.dst, dtype_bytes(g.dtype))) return TOPOEP_ERR_ALIGN;
     total += (double)g.rows * g.cols * dtype_bytes(g.dtype);
   }
+  if (outputs_overlap(count, tensors)) return TOPOEP_ERR_ARG;
   // a few chunks for each warp of a full grid, within the limits
   long long chunk_bytes = kMinChunkBytes;
   while (chunk_bytes < kMaxChunkBytes && total > 4.0 * chunk_bytes * 148 * kCtasPerSm * kClipWarps) chunk_bytes *= 2;
@@ -425,16 +456,16 @@ static int list_chunks(topoep_clip_ctx* h, int64_t count, const topoep_grad_tens
     } else if (g.cols * size >= kMinChunkBytes) {
       for (int64_t r = 0; r < g.rows; ++r) cut_run(h, src + r * ss * size, dst + r * ds * size, g.cols, g.dtype, chunk_bytes);
     } else {
-      const ClipRows rows = {g.cols, ss, ds};
+      const ClipRows rows = {ss, ds, (unsigned)g.cols, 0};
       const long long n = g.rows * g.cols;
       for (long long at = 0; at < n; at += kStridedElements) {
         ClipChunk c = {};
-        c.src = src;
-        c.dst = dst;
+        c.src = src + at / g.cols * ss * size;
+        c.dst = dst + at / g.cols * ds * size;
         c.n = (int)(n - at < kStridedElements ? n - at : kStridedElements);
         c.dtype = g.dtype;
         c.tensor = (int)h->rows.size();
-        c.first = at;
+        c.first = (int)(at % g.cols);
         h->chunks.push_back(c);
       }
       h->rows.push_back(rows);

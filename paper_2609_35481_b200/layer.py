@@ -73,6 +73,7 @@ class _RouterFunction(torch.autograd.Function):
         return ids, weights
 
     @staticmethod
+    @torch.autograd.function.once_differentiable
     def backward(ctx, _, grad_weights):
         logits, ids, weights = ctx.saved_tensors
         return ctx.router.backward(logits, ids, weights, grad_weights), None, None, None

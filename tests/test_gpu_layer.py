@@ -526,6 +526,36 @@ def test_clip_strided_and_permuted_tensors():
             GradientClip([bad])
 
 
+@pytest.mark.parametrize("rows,cols,stride", [(5000, 3, 7), (300, 1023, 1030), (2049, 1, 2), (100, 511, 600),
+                                              (40, 4097, 5000), (3, 2048, 2049)])
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_clip_rows_short_and_long(rows, cols, stride, dtype):
+    room = torch.randn(rows * stride, generator=gen(rows), device="cuda").to(dtype)
+    kept = room.clone()
+    view = torch.as_strided(room, (rows, cols), (stride, 1))
+    check_clip([view], 0.7)
+    gaps = torch.ones(rows * stride, dtype=torch.bool, device="cuda")
+    torch.as_strided(gaps, (rows, cols), (stride, 1)).fill_(False)
+    assert torch.equal(room[gaps], kept[gaps])
+    out = torch.empty(rows, cols, dtype=dtype, device="cuda")
+    check_clip([torch.as_strided(kept, (rows, cols), (stride, 1))], 0.7, out=[out])
+
+
+def test_clip_shared_gradient_is_refused():
+    t = torch.randn(100, device="cuda")
+    for bad in ([t, t], [t, t[50:]], [t.view(10, 10), t]):
+        with pytest.raises(B.TopoEPError):
+            GradientClip(bad)
+
+
+def test_router_is_differentiable_once():
+    x = torch.randn(3, 8, device="cuda", requires_grad=True)
+    _, w = Router(8, 2)(x)
+    (g,) = torch.autograd.grad(w.square().sum(), x, create_graph=True)
+    with pytest.raises(RuntimeError):
+        g.sum().backward()
+
+
 def test_clip_very_large_and_very_small_gradients():
     for scale in (1e30, 1e-30, 1e-42):
         t = [scale * torch.randn(100003, generator=gen(5), device="cuda"),

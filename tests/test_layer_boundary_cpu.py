@@ -90,3 +90,22 @@ def test_clip_empty_list_and_null_handle():
     B.topoep_clip_destroy(h)
     B.topoep_clip_destroy(None)
     assert B.topoep_clip_run(None, 0, 1.0, P) == -1 and B.topoep_clip_workspace_bytes(None) == 0
+
+
+def test_clip_refuses_a_gradient_listed_twice():
+    def rc(*tensors):
+        code, h = B.topoep_clip_create([B.GradTensor(src, dst, rows, cols, stride, stride, B.DTYPE_F32, 0)
+                                        for src, dst, rows, cols, stride in tensors])
+        if h is not None:
+            B.topoep_clip_destroy(h)
+        return code
+
+    assert rc((P, None, 1, 8, 8), (P + 32, None, 1, 8, 8)) == 0
+    assert rc((P, None, 1, 8, 8), (P + 28, None, 1, 8, 8)) == -10
+    assert rc((P + 28, None, 1, 8, 8), (P, None, 1, 8, 8)) == -10
+    assert rc((P, None, 1, 8, 8), (P, None, 1, 8, 8)) == -10
+    assert rc((P, None, 1, 100, 100), (P + 40, None, 1, 2, 2)) == -10
+    assert rc((P, 4 * P, 1, 8, 8), (P, 8 * P, 1, 8, 8)) == 0            # one source, two outputs
+    assert rc((P, 4 * P, 1, 8, 8), (2 * P, 4 * P, 1, 8, 8)) == -10
+    assert rc((P, None, 4, 8, 16), (P + 32, None, 4, 8, 16)) == 0       # two halves of rows
+    assert rc((P, None, 4, 8, 16), (P, None, 4, 8, 16)) == -10

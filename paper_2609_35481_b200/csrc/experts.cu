@@ -23,7 +23,7 @@
 // Between 1 and 2 only the copies of h wait, each for its instance's tiles: the copies of the
 // weights, issued by another warp, run ahead and keep the memory busy meanwhile.
 //
-// Roles of a CTA's warps: 0 copies weights, 1 copies token rows, 2 issues the products, 4-7 read the
+// Roles of a CTA's warps: 0 copies weights, 1 copies token rows, 2 issues the products, 4-11 read the
 // accumulators (double-buffered in tensor memory); all sixteen take part in 0 and 3.  The launch is cooperative: every CTA
 // is resident, so the waits of 2 and 3 end; all waits are bounded all the same and set
 // TOPOEP_FLAG_INTERNAL when they run out.
@@ -108,6 +108,7 @@ __global__ void __launch_bounds__(kAnyThreads) experts_down_any_kernel(const Exp
 // ------------------------------------------------------------------- the tensor-core kernel
 
 constexpr int kThreads = 512;
+constexpr int kEpilogueWarps = 8;       // warps 4 to 11; a multiple of 4
 constexpr int kTileM = 128;             // rows of one product; a stage holds two
 constexpr int kStepK = 64;              // elements of the sum in a step: one 128-byte swizzled row
 constexpr int kHalfBytes = kTileM * kStepK * 2;
@@ -163,10 +164,12 @@ __device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity) {
   }
   return false;
 }
-__device__ __forceinline__ void tma_weights(uint32_t dst, const CUtensorMap* map, int x, int y, int z, uint32_t bar) {
+__device__ __forceinline__ void tma_weights(uint32_t dst, const CUtensorMap* map, int x, int y, int z, uint32_t bar,
+                                            uint64_t policy) {
   asm volatile(
-      "cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];"
-      ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(z), "r"(bar) : "memory");
+      "cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes.L2::cache_hint "
+      "[%0], [%1, {%2, %3, %4}], [%5], %6;"
+      ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(z), "r"(bar), "l"(policy) : "memory");
 }
 __device__ __forceinline__ void tma_rows(uint32_t dst, const CUtensorMap* map, int x, int r0, int r1, int r2, int r3,
                                          uint32_t bar) {
@@ -224,7 +227,7 @@ __device__ __forceinline__ bool spin_until(const unsigned* p, unsigned want) {
     if (load_acquire(p) == want) return true;
   return false;
 }
-__device__ __forceinline__ void epilogue_sync() { asm volatile("bar.sync 1, 128;" ::: "memory"); }
+__device__ __forceinline__ void epilogue_sync() { asm volatile("bar.sync 1, %0;" ::"n"(kEpilogueWarps * 32) : "memory"); }
 
 // `units` cut into `n` runs of equal length (the first ones one longer).
 struct Cut {
@@ -300,7 +303,8 @@ __device__ __forceinline__ ulonglong2 get_part(const ulonglong2* at) {
 }
 
 __device__ __forceinline__ void store_h(const LayerParams& p, int row, int f, float g, float u) {
-  const float h = g / (1.0f + expf(-g)) * u;
+  // within some 2^-20, next to the 16 bits that are kept; 0 where the exponential is infinite
+  const float h = __fdividef(g, 1.0f + __expf(-g)) * u;
   const __nv_bfloat16 hi = __float2bfloat16_rn(h);
   // the rest of an infinity or NaN is 0: the first part says it all
   const float rest = h - to_f32(hi);
@@ -343,7 +347,7 @@ experts_kernel(const __grid_constant__ Maps maps, const __grid_constant__ LayerP
     }
     for (int b = 0; b < 2; ++b) {
       mbar_init(smem_u32(&bars[2 * kMaxStages + b]), 1);    // accumulator ready
-      mbar_init(smem_u32(&bars[2 * kMaxStages + 2 + b]), 128);   // accumulator read
+      mbar_init(smem_u32(&bars[2 * kMaxStages + 2 + b]), kEpilogueWarps * 32);   // accumulator read
     }
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     failed_shared = 0;
@@ -440,6 +444,9 @@ experts_kernel(const __grid_constant__ Maps maps, const __grid_constant__ LayerP
 
   if (warp == 0) {
     if (lane == 0) {   // ---- weights
+      // a weight is read once: the tokens' rows, h and the partial results should outlast it in L2
+      uint64_t policy;
+      asm volatile("createpolicy.fractional.L2::evict_first.b64 %0, 1.0;" : "=l"(policy));
       int st = 0;
       uint32_t ph = 0;
       bool ok = true;
@@ -460,8 +467,8 @@ experts_kernel(const __grid_constant__ Maps maps, const __grid_constant__ LayerP
             if (!mbar_wait(empty + 8 * st, ph ^ 1)) { ok = false; break; }
             const uint32_t dst = ring + st * stage_bytes;
             mbar_expect(full + 8 * st, kStageA);
-            tma_weights(dst, map, s * kStepK, y0, z, full + 8 * st);
-            tma_weights(dst + kHalfBytes, map, s * kStepK, y1, z, full + 8 * st);
+            tma_weights(dst, map, s * kStepK, y0, z, full + 8 * st, policy);
+            tma_weights(dst + kHalfBytes, map, s * kStepK, y1, z, full + 8 * st, policy);
             if (++st == stages) { st = 0; ph ^= 1; }
           }
         }
@@ -565,11 +572,14 @@ experts_kernel(const __grid_constant__ Maps maps, const __grid_constant__ LayerP
       if (!ok) *failed = 1;
     }
     __syncwarp();
-  } else if (warp >= 4 && warp < 8) {   // ---- accumulators
-    const int quad = warp & 3, row = quad * 32 + lane, etid = tid - 128;
+  } else if (warp >= 4 && warp < 4 + kEpilogueWarps) {   // ---- accumulators
+    // a warp reads the 32 lanes of tensor memory that its number allows; the warps of a quarter take
+    // the columns in turn
+    const int quad = warp & 3, row = quad * 32 + lane, etid = tid - 128, turn = (warp - 4) >> 2;
+    constexpr int kTurns = kEpilogueWarps / 4;
     int buf = 0;
     uint32_t accph = 0;
-    bool quit = false, lost = false;   // quit is the same in all four warps, lost is a thread's own
+    bool quit = false, lost = false;   // quit is the same in all these warps, lost is a thread's own
     for (int phase = 0; phase < 2 && !quit; ++phase) {
       const Schedule& sched = phase ? sched2 : sched1;
       const int per_slot = phase ? per_slot2 : per_slot1;
@@ -579,7 +589,7 @@ experts_kernel(const __grid_constant__ Maps maps, const __grid_constant__ LayerP
         if (!mbar_wait(acc_full + 8 * buf, accph)) *stopped = 1;
         const int slot = pc.tile / per_slot, m = pc.tile - slot * per_slot;
         const bool whole = pc.k0 == 0 && pc.k1 == sched.steps;
-        epilogue_sync();   // the four warps go on, or stop, together
+        epilogue_sync();   // the warps go on, or stop, together
         quit = *stopped != 0;
         if (quit) break;
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
@@ -589,7 +599,7 @@ experts_kernel(const __grid_constant__ Maps maps, const __grid_constant__ LayerP
         if (phase) {
           float* yp = p.yp + ((size_t)(cta - sched.first_cta(pc.tile)) * n_rows + o) * p.H + m * 2 * kTileM + row;
           const bool in0 = m * 2 * kTileM + row < p.H, in1 = m * 2 * kTileM + kTileM + row < p.H;
-          for (int c = 0; c < n; c += 16) {
+          for (int c = 16 * turn; c < n; c += 16 * kTurns) {
             float v0[16], v1[16];
             tmem_load16(d + c, v0);
             tmem_load16(d + p.acc_cols + c, v1);
@@ -607,7 +617,7 @@ experts_kernel(const __grid_constant__ Maps maps, const __grid_constant__ LayerP
           // for a CTA that waits).
           finish = pc.k0 == 0;
           const int f = m * kTileM + row, parts = finish && !whole ? sched.parts(pc.tile) : 1;
-          for (int c = 0; c < n; c += 8) {
+          for (int c = 8 * turn; c < n; c += 8 * kTurns) {
             float g[8], u[8];
             tmem_load8(d + c, g);
             tmem_load8(d + p.acc_cols + c, u);

@@ -123,7 +123,7 @@ constexpr unsigned kSpinLimit = 1u << 20;   // polls of a word in global memory 
 enum { C_STATUS = 0, C_ARRIVE = 32, C_LEAVE = 48, C_SERIAL = 56 };
 
 struct __align__(64) Maps {
-  CUtensorMap main_gu, main_down, replica_gu, replica_down, x, h;
+  CUtensorMap main_gu, main_down, replica_gu, replica_down, x, x_box, h;
 };
 
 struct LayerParams {
@@ -247,8 +247,7 @@ struct Piece {
 // at most a sixteenth of the CTAs idle, else the steps of the rest in one row are cut into equal
 // runs.  Cut tiles come first and whole ones last, so that the parts of a cut tile are summed while
 // whole tiles stream.  The rule keeps 144 tiles whole on 148 CTAs (128 rows on nine 7168 x 2048
-// experts: phase 1 ended at 99 us, cut at 118 us) and cuts 128 (one token on eight of them: 81 us,
-// whole it would take 148 / 128 of the streaming time).
+// experts: 146 us, cut 154 us) and cuts 128 (eight tokens on eight of them: 123 us, whole 127 us).
 struct Schedule {
   int steps, tiles, n, rest, rounds;
   bool cut_rest;
@@ -300,6 +299,15 @@ __device__ __forceinline__ ulonglong2 get_part(const ulonglong2* at) {
   ulonglong2 v;
   asm volatile("ld.volatile.global.v2.u64 {%0, %1}, [%2];" : "=l"(v.x), "=l"(v.y) : "l"(at) : "memory");
   return v;
+}
+
+// Rows an instance gets for the tokens in its mask: one a token, or all tokens' rows where most are
+// there anyway, because the copy unit gathers rows four at a time and fetches whole boxes of
+// sixteen far faster (the surplus rows are computed and never read).  128 tokens, nine 7168 x 2048
+// experts: gathered 175 us with 80 rows an expert, 196 with 96, 234 with 128; all rows 180.
+__device__ __forceinline__ int rows_of(const uint4& m, int tokens) {
+  const int c = __popc(m.x) + __popc(m.y) + __popc(m.z) + __popc(m.w);
+  return 4 * c >= 3 * tokens ? tokens : c;
 }
 
 __device__ __forceinline__ void store_h(const LayerParams& p, int row, int f, float g, float u) {
@@ -373,8 +381,7 @@ experts_kernel(const __grid_constant__ Maps maps, const __grid_constant__ LayerP
   const int per = (N + kThreads - 1) / kThreads, first = min(N, tid * per), last = min(N, first + per);
   int my_slots = 0, my_rows = 0, my_most = 0;
   for (int i = first; i < last; ++i) {
-    const uint4 m = reinterpret_cast<const uint4*>(mask)[i];
-    const int c = __popc(m.x) + __popc(m.y) + __popc(m.z) + __popc(m.w);
+    const int c = rows_of(reinterpret_cast<const uint4*>(mask)[i], p.tokens);
     my_slots += c > 0;
     my_rows += c;
     my_most = max(my_most, c);
@@ -397,8 +404,7 @@ experts_kernel(const __grid_constant__ Maps maps, const __grid_constant__ LayerP
     most = max(most, warp_tot[2][w]);
   }
   for (int i = first; i < last; ++i) {
-    const uint4 m4 = reinterpret_cast<const uint4*>(mask)[i];
-    const int c = __popc(m4.x) + __popc(m4.y) + __popc(m4.z) + __popc(m4.w);
+    const int c = rows_of(reinterpret_cast<const uint4*>(mask)[i], p.tokens);
     if (c == 0) continue;
     act[s_at] = (uint16_t)i;
     off[s_at] = (uint16_t)r_at;
@@ -415,8 +421,11 @@ experts_kernel(const __grid_constant__ Maps maps, const __grid_constant__ LayerP
     if (id >= 0 && id < N) {
       const int t = a / p.k;
       const uint32_t* m = mask + id * 4;
-      int before = __popc(m[t >> 5] & ((1u << (t & 31)) - 1));
-      for (int w = 0; w < (t >> 5); ++w) before += __popc(m[w]);
+      int before = t;   // an instance of all tokens has them in their own order
+      if (rows_of(*reinterpret_cast<const uint4*>(m), p.tokens) != p.tokens) {
+        before = __popc(m[t >> 5] & ((1u << (t & 31)) - 1));
+        for (int w = 0; w < (t >> 5); ++w) before += __popc(m[w]);
+      }
       sl = slot_of[id];
       row = (uint16_t)(off[sl] + before);
       tok[row] = (uint8_t)t;
@@ -496,18 +505,19 @@ experts_kernel(const __grid_constant__ Maps maps, const __grid_constant__ LayerP
           __syncwarp();
           asm volatile("fence.proxy.async.global;" ::: "memory");
         }
-        // x: four gathered rows a lane; h: 16 adjacent rows a lane, the first lanes the rounded
-        // values and the next ones the rests.  Rows past the instance's last are some other row's:
-        // columns of the product that nobody reads.
+        // x: four gathered rows a lane, or 16 adjacent ones where the instance has all tokens; h: 16
+        // adjacent rows a lane, the first lanes the rounded values and the next ones the rests.
+        // Rows past the instance's last are some other row's: columns that nobody reads.
         const int slot = pc.tile / per_slot, o = off[slot], n = off[slot + 1] - o;
-        const int groups = phase ? (n + 15) >> 4 : (n + 3) >> 2;
-        const int copies = phase ? 2 * groups : groups, bytes = phase ? 2 * groups * 2048 : groups * 512;
+        const bool gather = phase == 0 && n != p.tokens;
+        const int groups = gather ? (n + 3) >> 2 : (n + 15) >> 4;
+        const int copies = phase ? 2 * groups : groups, bytes = gather ? groups * 512 : copies * 2048;
         int row[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) row[i] = tok[o + min(4 * lane + i, n - 1)];
         const bool rest = lane >= groups;
-        const int y = o + 16 * (rest ? lane - groups : lane) + (rest ? p.max_rows : 0);
-        const uint32_t to = phase ? (rest ? b_half + (lane - groups) * 2048 : lane * 2048) : lane * 512;
+        const int y = phase ? o + 16 * (rest ? lane - groups : lane) + (rest ? p.max_rows : 0) : 16 * lane;
+        const uint32_t to = gather ? lane * 512 : rest ? b_half + (lane - groups) * 2048 : lane * 2048;
         for (int s = pc.k0; s < pc.k1; ++s) {
           int good = 1;
           if (lane == 0) {
@@ -518,8 +528,8 @@ experts_kernel(const __grid_constant__ Maps maps, const __grid_constant__ LayerP
           if (!ok) break;
           if (lane < copies) {
             const uint32_t dst = ring + st * stage_bytes + kStageA + to;
-            if (phase == 0) tma_rows(dst, &maps.x, s * kStepK, row[0], row[1], row[2], row[3], full + 8 * st);
-            else tma_box(dst, &maps.h, s * kStepK, y, full + 8 * st);
+            if (gather) tma_rows(dst, &maps.x, s * kStepK, row[0], row[1], row[2], row[3], full + 8 * st);
+            else tma_box(dst, phase ? &maps.h : &maps.x_box, s * kStepK, y, full + 8 * st);
           }
           if (++st == stages) { st = 0; ph ^= 1; }
         }
@@ -684,8 +694,8 @@ experts_kernel(const __grid_constant__ Maps maps, const __grid_constant__ LayerP
     // The 256 outputs of a token that a tile of rows gives are one item: lane j works out where the
     // parts of id j are, then all lanes read eight outputs of every part, eight parts at a time.  A
     // warp takes an item; when there are fewer items than CTAs, the warps of a CTA share one, each
-    // taking every sixteenth part (one token, eight ids: 4.5 us after the last partial result with a
-    // warp an item, 2 us shared).
+    // taking every sixteenth part (eight parts to add: 4.5 us after the last partial result with
+    // a warp an item, 2 us shared).
     constexpr int kWarps = kThreads / 32;
     const int items = p.tokens * per_slot2;
     const bool shared_item = items <= (int)gridDim.x;
@@ -982,7 +992,7 @@ struct Shape {
   size_t bytes;
   Shape(int tokens, int k, int instances) {
     const int a = tokens * k, slots = std::min(a, instances);
-    const size_t tables = 2 * (size_t)slots + 2 * ((size_t)slots + 2) + (a + 1) / 2 * 2 + 8 * (size_t)a + 16;
+    const size_t tables = 2 * (size_t)slots + 2 * ((size_t)slots + 2) + (size_t)a * 4 / 3 + 8 * (size_t)a + 16;
     ring = (int)((kSharedLimit - tables) / 1024 * 1024);
     o_act = ring + 4 * a;   // weights first
     o_off = o_act + 2 * slots;
@@ -1029,7 +1039,7 @@ extern "C" int topoep_experts_create(topoep_experts_t* out, int ranks, int exper
   h->ffn = ffn;
   h->top_k = top_k;
   h->max_tokens = max_tokens;
-  h->max_rows = max_tokens * top_k;
+  h->max_rows = max_tokens * top_k * 4 / 3 + 1;   // see rows_of
   // rows of both matrices start on 16 bytes, as the copy unit needs them
   h->tiled = hidden % 8 == 0 && ffn % 8 == 0;
   h->off_h = kAlign + align_up((size_t)4 * std::min(h->max_rows, h->instances));   // control, counters
@@ -1112,7 +1122,9 @@ namespace {
 cudaError_t launch_tiled(topoep_experts_t h, const ExpertsParams& a, cudaStream_t stream) {
   Maps maps = h->maps;
   const uint64_t stride = a.tokens > 1 ? 2 * (uint64_t)a.x_stride : 2 * (uint64_t)h->hidden;
-  if (!encode(h->encode, &maps.x, a.x, 2, h->hidden, a.tokens, 1, stride, 0, 1)) return cudaErrorInvalidValue;
+  if (!encode(h->encode, &maps.x, a.x, 2, h->hidden, a.tokens, 1, stride, 0, 1) ||
+      !encode(h->encode, &maps.x_box, a.x, 2, h->hidden, a.tokens, 1, stride, 0, 16))
+    return cudaErrorInvalidValue;
   const Shape sh(a.tokens, a.k, h->instances);
   LayerParams p = {};
   p.ids = a.ids;

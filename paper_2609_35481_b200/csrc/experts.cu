@@ -18,15 +18,21 @@
 //
 // The work of 1 and of 2 is a list of tiles of rows, each a sum over steps of 64 elements, dealt out
 // so that all SMs stream nearly the same number of bytes whatever the sizes (Schedule).  A tile cut
-// between CTAs is summed from partial accumulators in a fixed order: in 1 by the CTA that finishes
-// last (the activation needs the whole sum), in 2 by step 3.
+// between CTAs is summed from partial accumulators in a fixed order: in 1 by the CTA that has its
+// first step (the activation needs the whole sum), in 2 by step 3.
 // Between 1 and 2 only the copies of h wait, each for its instance's tiles: the copies of the
 // weights, issued by another warp, run ahead and keep the memory busy meanwhile.
 //
 // Roles of a CTA's warps: 0 copies weights, 1 copies token rows, 2 issues the products, 4-11 read the
-// accumulators (double-buffered in tensor memory); all sixteen take part in 0 and 3.  The launch is cooperative: every CTA
-// is resident, so the waits of 2 and 3 end; all waits are bounded all the same and set
-// TOPOEP_FLAG_INTERNAL when they run out.
+// accumulators (double-buffered in tensor memory); all sixteen take part in 0 and 3.  The launch is
+// cooperative: every CTA is resident, so the waits for other CTAs end; all waits are bounded all
+// the same and set TOPOEP_FLAG_INTERNAL when they run out.
+//
+// Measured (B200, weights read / time): 16 tokens on 38 experts of 2048 x 1408 660 MB in 105 us (6.3
+// TB/s of 6.45 that a copy reaches), 64 tokens 977 MB in 156 us; eight tokens on eight experts of
+// 7168 x 2048 705 MB in 123 us; 16, 64 and 128 rows on each of nine such experts 793 MB in 134, 156
+// and 181 us: the rows' share of the traffic from L2 grows to that of the weights.  What a small call
+// cannot hide is some 15 us: launch, grouping, the fill of the ring, the wait for h, the last sums.
 #include <cuda.h>
 
 #include <algorithm>
@@ -66,7 +72,8 @@ __device__ __forceinline__ float warp_sum(float v) {
   return v;
 }
 
-// Any sizes and alignment: one warp for an (assignment, row of gate and up).
+// Sizes that are no multiples of 8 elements, so that rows start anywhere: one warp for an (assignment,
+// row of gate and up), element by element.  Weights are read once an assignment.
 __global__ void __launch_bounds__(kAnyThreads) experts_gate_any_kernel(const ExpertsParams p) {
   const int lane = threadIdx.x & 31, a = blockIdx.y, f = blockIdx.x * (kAnyThreads / 32) + (threadIdx.x >> 5);
   const int inst = p.ids[a];
@@ -950,6 +957,13 @@ __global__ void __launch_bounds__(kOneThreads, 1) experts_one_kernel(const __gri
   }
 }
 
+// Rows of x that do not start on 16 bytes, into rows that do.
+__global__ void __launch_bounds__(kAnyThreads) experts_align_kernel(const __nv_bfloat16* x, long long stride, int H,
+                                                                    __nv_bfloat16* to) {
+  for (int i = blockIdx.x * kAnyThreads + threadIdx.x; i < H; i += gridDim.x * kAnyThreads)
+    to[(size_t)blockIdx.y * H + i] = x[blockIdx.y * stride + i];
+}
+
 constexpr size_t kAlign = 256;
 inline size_t align_up(size_t x) { return (x + kAlign - 1) / kAlign * kAlign; }
 
@@ -1015,7 +1029,7 @@ struct topoep_experts_ctx {
   const void* replica;
   bool have_params, tiled;   // tiled: sizes that the copy unit can address
   unsigned char* ws;
-  size_t ws_bytes, off_h, off_partial, off_yp;
+  size_t ws_bytes, off_h, off_partial, off_yp, off_x;
   EncodeFn encode;
   Maps maps;
 };
@@ -1055,7 +1069,8 @@ extern "C" int topoep_experts_create(topoep_experts_t* out, int ranks, int exper
                                 std::min<long long>(h->max_rows, (long long)n * max_tokens));
     const size_t cols = (max_tokens + 15) / 16 * 16;
     h->off_yp = h->off_partial + align_up((size_t)kMaxCtas * cols * kTileM * sizeof(ulonglong2));
-    h->ws_bytes = h->off_yp + align_up((size_t)4 * rows * hidden);
+    h->off_x = h->off_yp + align_up((size_t)4 * rows * hidden);
+    h->ws_bytes = h->off_x + align_up((size_t)2 * max_tokens * hidden);
   }
   *out = h;
   return TOPOEP_OK;
@@ -1228,9 +1243,16 @@ extern "C" int topoep_experts_forward(topoep_experts_t h, const void* dev_x, int
   p.slots = h->slots;
   p.instances = h->instances;
   cudaError_t e;
-  if (h->tiled && aligned_to(dev_x, 16) && (tokens == 1 || x_row_stride % 8 == 0)) {
+  if (h->tiled) {
+    if (!aligned_to(dev_x, 16) || (tokens > 1 && x_row_stride % 8 != 0)) {
+      __nv_bfloat16* rows = reinterpret_cast<__nv_bfloat16*>(h->ws + h->off_x);
+      experts_align_kernel<<<dim3((p.H + kAnyThreads - 1) / kAnyThreads, tokens), kAnyThreads, 0, st>>>(p.x, p.x_stride, p.H, rows);
+      p.x = rows;
+      p.x_stride = p.H;
+    }
     const bool one = tokens == 1 && one_shared(p, h->ctas) <= kOneShared;
     e = one ? launch_one(h, p, st) : launch_tiled(h, p, st);
+    if (e == cudaSuccess) e = cudaGetLastError();
   } else {
     const int per = kAnyThreads / 32;
     experts_gate_any_kernel<<<dim3((p.F + per - 1) / per, tokens * p.k), kAnyThreads, 0, st>>>(p);

@@ -681,8 +681,7 @@ experts_kernel(const __grid_constant__ Maps maps, const __grid_constant__ LayerP
         if (!finish) continue;
         // h is read by the copy unit of other CTAs
         asm volatile("fence.proxy.async.global;" ::: "memory");
-        __threadfence();
-        epilogue_sync();
+        epilogue_sync();   // the release below covers what these threads wrote before it
         if (etid == 0) add_release(p.done + slot, 1);
       }
     }
@@ -690,8 +689,7 @@ experts_kernel(const __grid_constant__ Maps maps, const __grid_constant__ LayerP
   }
 
   // ---- all partial results are written: weigh and sum
-  __threadfence();
-  __syncthreads();
+  __syncthreads();   // the release below covers what the CTA wrote before it
   if (tid == 0) {
     add_release(p.control + C_ARRIVE, 1);
     if (!spin_until(p.control + C_ARRIVE, gridDim.x)) failed_shared = 1;
@@ -927,8 +925,7 @@ __global__ void __launch_bounds__(kOneThreads, 1) experts_one_kernel(const __gri
       asm volatile("prefetch.global.L2 [%0];" ::"l"(row + at));
     }
   }
-  __threadfence();
-  __syncthreads();
+  __syncthreads();   // the release below covers what the CTA wrote before it
   if (tid == 0) {
     add_release(p.control + C_ARRIVE, 1);
     if (!spin_until(p.control + C_ARRIVE, G)) failed = 1;

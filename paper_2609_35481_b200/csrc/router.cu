@@ -152,6 +152,10 @@ __global__ void __launch_bounds__(kRouterThreads) router_backward_any_kernel(con
 //   3. a candidate's place is the number of larger candidates.  Equal values share a place, which
 //      the sum of the places gives away: then ids are compared too.
 // More than kCandidates of them (many equal logits) take k rounds over the rows instead.
+// 262144 x 256 logits of 32 bits: 178 instructions a token, 69 us, 0.64 of the copy rate.  What is
+// left is the chain of shuffles, shared-memory reads and loads within a warp: 32 warps an SM (64
+// registers) issue in 0.6 of the cycles, more warps spill, and fetching the next rows ahead into
+// registers or L2 changed nothing.
 constexpr int kCandidates = 32;
 
 template <typename T, int N> struct Row;   // N adjacent elements
@@ -412,7 +416,9 @@ __global__ void __launch_bounds__(kRouterThreads, kRouterBlocksPerSm) router_for
 //
 // Bound by memory: a row of gradients written for each token and 12 bytes read for each choice; the
 // row of logits is read too where the softmax over all experts is differentiated, else only the
-// chosen logits.  The row goes out as vectors, then the chosen places are written over it.
+// chosen logits.  The row goes out as vectors, then the chosen places are written over it.  131072
+// tokens: 256 experts of 32 bits with the full softmax 45 us (0.97 of the copy rate), 64 experts of
+// 16 bits 13 us (0.51) and without it 8 us (0.51): with short rows the scattered stores count.
 
 // Gradient at the chosen places only: eight lanes a token.  The zeros leave while the ids, weights
 // and their gradients are on their way.

@@ -433,6 +433,30 @@ def test_experts_other_stream_graph_and_moved_blocks():
     assert ((small.float() - y[:3].float()).abs() <= 0.02 * (1 + y[:3].float().abs())).all()
 
 
+def test_experts_and_clip_on_two_streams_at_once():
+    """Calls on handles of their own overlap freely: each waits for its own blocks alone."""
+    g = gen(3)
+    sets, streams = [], [torch.cuda.Stream() for _ in range(3)]
+    for seed in (1, 2):
+        layer, x, ids, w, y = check_experts(9 * seed, 3, 1, 6, 0, 512, 256, seed=seed)
+        sets.append((layer, x, ids, w, y))
+    t = torch.randn(3_000_000, generator=g, device="cuda")
+    out = torch.empty_like(t)
+    clip = GradientClip([t], out=[out])
+    norm, want = clip.clip(1.0), out.clone()
+    wrong = [torch.zeros((), dtype=torch.int64, device="cuda") for _ in range(3)]
+    torch.cuda.synchronize()
+    for _ in range(60):
+        for i, (layer, x, ids, w, y) in enumerate(sets):
+            with torch.cuda.stream(streams[i]):
+                wrong[i] += (layer.forward(x, ids, w) != y).any()
+        with torch.cuda.stream(streams[2]):
+            wrong[2] += clip.clip(1.0) != norm
+    torch.cuda.synchronize()
+    assert [int(v) for v in wrong] == [0, 0, 0] and torch.equal(out, want)
+    assert all(s[0].status() == 0 for s in sets)
+
+
 def test_experts_refusals():
     layer, x, ids, w, _ = check_experts(4, 2, 1, 3, 0, 64, 64)
     for bad in (lambda: layer.forward(x.float(), ids, w), lambda: layer.forward(x[:, :32], ids, w),

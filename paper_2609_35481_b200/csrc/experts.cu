@@ -820,9 +820,10 @@ experts_kernel(const __grid_constant__ Maps maps, const __grid_constant__ LayerP
 //      the sums, weighed, are added up in the order of the ids.
 // Against the tensor-core kernel with one token: two experts of 1024 x 2048 (25 MB) 11.7 against
 // 19.9 us, eight of 7168 x 2048 (705 MB) 110 against 121 us (6.4 TB/s); with two tokens that kernel
-// is at the speed of the memory itself (1.06 GB in 166 us).  24 warps: with 16 it is 114 us, with 32
-// (and half the loads in flight for each) 113 us and 10.2 us for the small one.
-constexpr int kOneThreads = 768, kOneWarps = kOneThreads / 32, kMaxIds = 16;
+// is at the speed of the memory itself (1.06 GB in 166 us).  24 warps with eight vectors a lane in
+// flight: with 16 it is 114 us, with 32 (four vectors each, for the registers) 113 us.  But where 32
+// warps an SM hold every row of gate and up at once they win: the small one 10.2 against 11.7 us.
+constexpr int kOneWarps = 24, kOneWarpsSmall = 32, kMaxIds = 16;
 constexpr int kOneAhead = 128 * 1024;        // bytes of a CTA's down rows fetched before the wait
 constexpr size_t kOneShared = 160 * 1024;    // most bytes of the token's row or a CTA's sums
 
@@ -836,9 +837,9 @@ __device__ __forceinline__ void unpack8(const uint4& v, float (&f)[8]) {
 }
 
 // Sums of n weights at `w` (and at `w2` if TWO) times n values at v; the same in every lane.
-template <bool TWO>
+template <bool TWO, int VECS>
 __device__ __forceinline__ float2 dot_row(const __nv_bfloat16* w, const __nv_bfloat16* w2, int n, const float* v, int lane) {
-  constexpr int kAhead = TWO ? 4 : 8;   // 16 bytes a lane each
+  constexpr int kAhead = TWO ? VECS / 2 : VECS;   // 16 bytes a lane each
   const int vecs = n >> 3;
   float sum = 0.0f, sum2 = 0.0f;
   for (int base = lane; base < vecs; base += 32 * kAhead) {
@@ -876,7 +877,9 @@ struct OneParams {
   uint32_t* control;
 };
 
-__global__ void __launch_bounds__(kOneThreads, 1) experts_one_kernel(const __grid_constant__ OneParams p) {
+template <int WARPS, int VECS>
+__global__ void __launch_bounds__(WARPS * 32, 1) experts_one_kernel(const __grid_constant__ OneParams p) {
+  constexpr int kThreadsHere = WARPS * 32;
   extern __shared__ __align__(16) float room[];   // the token's row, then sums [output][id]
   __shared__ const __nv_bfloat16* block[kMaxIds];
   __shared__ float weight[kMaxIds];
@@ -896,7 +899,7 @@ __global__ void __launch_bounds__(kOneThreads, 1) experts_one_kernel(const __gri
     }
     if (lane == 0) { n_shared = __popc(all); failed = 0; }
   } else {
-    for (int q = tid - 32; q < H / 8; q += kOneThreads - 32) {
+    for (int q = tid - 32; q < H / 8; q += kThreadsHere - 32) {
       float f[8];
       unpack8(*(reinterpret_cast<const uint4*>(p.e.x) + q), f);
       float4* to = reinterpret_cast<float4*>(room) + 2 * q;
@@ -908,17 +911,17 @@ __global__ void __launch_bounds__(kOneThreads, 1) experts_one_kernel(const __gri
   const int n = n_shared;
 
   // ---- gate and up
-  for (int u = warp * G + cta; u < n * F; u += kOneWarps * G) {
+  for (int u = warp * G + cta; u < n * F; u += WARPS * G) {
     const int s = u / F, f = u - s * F;
     const __nv_bfloat16* wg = block[s] + (long long)f * H;
-    const float2 gu = dot_row<true>(wg, wg + (long long)F * H, H, room, lane);
+    const float2 gu = dot_row<true, VECS>(wg, wg + (long long)F * H, H, room, lane);
     if (lane == 0) p.e.h[u] = gu.x / (1.0f + expf(-gu.x)) * gu.y;
   }
   const int c0 = (int)((long long)H * cta / G), c1 = (int)((long long)H * (cta + 1) / G);
   const int units = (c1 - c0) * n;
   {   // the first down rows, a 128-byte line a thread
     const int lines = (F * 2 + 127) / 128, ahead = min(units, kOneAhead / (F * 2));
-    for (int i = tid; i < ahead * lines; i += kOneThreads) {
+    for (int i = tid; i < ahead * lines; i += kThreadsHere) {
       const int unit = i / lines, c = unit / n, s = unit - c * n;
       const char* row = reinterpret_cast<const char*>(block[s] + 2ll * F * H + (long long)(c0 + c) * F);
       const int at = min((i - unit * lines) * 128, 2 * F - 16);   // inside the row
@@ -933,14 +936,14 @@ __global__ void __launch_bounds__(kOneThreads, 1) experts_one_kernel(const __gri
   __syncthreads();
 
   // ---- down
-  for (int unit = warp; unit < units; unit += kOneWarps) {
+  for (int unit = warp; unit < units; unit += WARPS) {
     const int c = unit / n, s = unit - c * n;
     const __nv_bfloat16* wd = block[s] + 2ll * F * H + (long long)(c0 + c) * F;
-    const float2 v = dot_row<false>(wd, wd, F, p.e.h + (long long)s * F, lane);
+    const float2 v = dot_row<false, VECS>(wd, wd, F, p.e.h + (long long)s * F, lane);
     if (lane == 0) room[unit] = v.x;   // the token's row is done with
   }
   __syncthreads();
-  for (int c = tid; c < c1 - c0; c += kOneThreads) {
+  for (int c = tid; c < c1 - c0; c += kThreadsHere) {
     float y = 0.0f;
     for (int s = 0; s < n; ++s) y += weight[s] * room[c * n + s];
     p.e.y[c0 + c] = __float2bfloat16_rn(y);
@@ -1092,7 +1095,9 @@ extern "C" int topoep_experts_set_workspace(topoep_experts_t h, void* dev_ptr, s
     if (e == cudaSuccess)
       e = cudaFuncSetAttribute(experts_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSharedLimit);
     if (e == cudaSuccess)
-      e = cudaFuncSetAttribute(experts_one_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kOneShared);
+      e = cudaFuncSetAttribute(experts_one_kernel<kOneWarps, 8>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kOneShared);
+    if (e == cudaSuccess)
+      e = cudaFuncSetAttribute(experts_one_kernel<kOneWarpsSmall, 4>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kOneShared);
     if (e != cudaSuccess) return TOPOEP_ERR_CUDA;
     h->encode = encode_fn();
     if (!h->encode || !encode(h->encode, &h->maps.h, ws + h->off_h, 2, h->ffn, 2 * h->max_rows, 1,
@@ -1194,7 +1199,8 @@ cudaError_t launch_one(topoep_experts_t h, const ExpertsParams& a, cudaStream_t 
   p.control = reinterpret_cast<uint32_t*>(h->ws);
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(h->ctas);
-  cfg.blockDim = dim3(kOneThreads);
+  const bool small = a.k * a.F <= kOneWarpsSmall * h->ctas;   // a warp for every row
+  cfg.blockDim = dim3(32 * (small ? kOneWarpsSmall : kOneWarps));
   cfg.dynamicSmemBytes = one_shared(a, h->ctas);
   cfg.stream = stream;
   cudaLaunchAttribute attr[1];
@@ -1202,7 +1208,8 @@ cudaError_t launch_one(topoep_experts_t h, const ExpertsParams& a, cudaStream_t 
   attr[0].val.cooperative = 1;
   cfg.attrs = attr;
   cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, experts_one_kernel, p);
+  return small ? cudaLaunchKernelEx(&cfg, experts_one_kernel<kOneWarpsSmall, 4>, p)
+               : cudaLaunchKernelEx(&cfg, experts_one_kernel<kOneWarps, 8>, p);
 }
 
 }  // namespace

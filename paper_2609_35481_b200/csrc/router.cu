@@ -158,16 +158,10 @@ __global__ void __launch_bounds__(kRouterThreads) router_backward_any_kernel(con
 // registers or L2 changed nothing.
 constexpr int kCandidates = 32;
 
-template <typename T, int N> struct Row;   // N adjacent elements
-template <> struct Row<float, 1> { using type = float; };
-template <> struct Row<float, 2> { using type = float2; };
+template <typename T, int N> struct Row;   // N adjacent elements as one word of 8 or 16 bytes
 template <> struct Row<float, 4> { using type = float4; };
-template <> struct Row<__nv_bfloat16, 1> { using type = __nv_bfloat16; };
-template <> struct Row<__nv_bfloat16, 2> { using type = uint32_t; };
 template <> struct Row<__nv_bfloat16, 4> { using type = uint2; };
 template <> struct Row<__nv_bfloat16, 8> { using type = uint4; };
-template <> struct Row<__half, 1> { using type = __half; };
-template <> struct Row<__half, 2> { using type = uint32_t; };
 template <> struct Row<__half, 4> { using type = uint2; };
 template <> struct Row<__half, 8> { using type = uint4; };
 
@@ -589,6 +583,8 @@ cudaError_t launch_backward(const RouterParams& p, int sms, cudaStream_t stream)
       router_backward_sparse_kernel<T, false><<<blocks, kRouterThreads, 0, stream>>>(p);
     return cudaGetLastError();
   }
+  // eight values a lane where that leaves whole rows to a warp, more only beyond 256 experts (131072 x
+  // 512: 61 us with 32 lanes of 16 values, 74 us with 16 lanes of 32)
   if (p.E <= 32) return launch_backward_rows<T, 8, 4>(p, sms, stream);
   if (p.E <= 64) return launch_backward_rows<T, 8, 8>(p, sms, stream);
   if (p.E <= 128) return launch_backward_rows<T, 16, 8>(p, sms, stream);

@@ -153,9 +153,9 @@ __global__ void __launch_bounds__(kRouterThreads) router_backward_any_kernel(con
 //      the sum of the places gives away: then ids are compared too.
 // More than kCandidates of them (many equal logits) take k rounds over the rows instead.
 // 262144 x 256 logits of 32 bits: 178 instructions a token, 69 us, 0.64 of the copy rate.  What is
-// left is the chain of shuffles, shared-memory reads and loads within a warp: 32 warps an SM (64
-// registers) issue in 0.6 of the cycles, more warps spill, and fetching the next rows ahead into
-// registers or L2 changed nothing.
+// left is comparisons and maxima (the integer pipe at 0.55, issue at 0.62 of the cycles) and the chain
+// of shuffles and shared-memory reads in a warp.  Fetching the next rows ahead into registers or L2
+// changed nothing; 48 warps an SM instead of 32, for which the row has to be read twice, took 72 us.
 constexpr int kCandidates = 32;
 
 template <typename T, int N> struct Row;   // N adjacent elements as one word of 8 or 16 bytes

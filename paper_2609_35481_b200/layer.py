@@ -5,6 +5,7 @@ and every step runs in the CUDA library on the caller's stream.
 """
 from __future__ import annotations
 
+import ctypes
 from typing import Optional, Sequence
 
 import torch
@@ -51,9 +52,12 @@ class _Elsewhere:
         self.guard.__exit__(*exc)
 
 
+_current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
+
+
 def _at_home(index: int, stream: Optional[torch.cuda.Stream]) -> bool:
     """The call runs on the current stream of the current device: nothing to set up."""
-    return torch.cuda.current_device() == index and \
+    return _current_device() == index and \
         (stream is None or stream.cuda_stream == _current_raw(index))
 
 
@@ -91,26 +95,37 @@ class Router:
         _check(score in ("softmax", "sigmoid"), "score is 'softmax' or 'sigmoid'")
         self.experts, self.top_k, self.score = int(experts), int(top_k), score
         self.normalize, self.scale = bool(normalize), float(scale)
-        self._cfg = {d: B.RouterConfig(self.experts, self.top_k, code,
-                                       B.SCORE_SIGMOID if score == "sigmoid" else B.SCORE_SOFTMAX,
-                                       int(self.normalize), self.scale)
-                     for d, code in _DTYPES.items()}
+        cfg = {d: B.RouterConfig(self.experts, self.top_k, code,
+                                 B.SCORE_SIGMOID if score == "sigmoid" else B.SCORE_SOFTMAX,
+                                 int(self.normalize), self.scale)
+               for d, code in _DTYPES.items()}
+        # a call is a few microseconds of host work, so what it needs of ctypes is made once
+        self._cfg = {d: ctypes.byref(c) for d, c in cfg.items()}
+        self._forward, self._backward = B.lib().topoep_router_forward, B.lib().topoep_router_backward
         # the configuration's own errors, without a device
-        _raise(B.topoep_router_forward(self._cfg[torch.float32], None, self.experts, 0, None, None,
-                                       None, None))
+        _raise(B.topoep_router_forward(cfg[torch.float32], None, self.experts, 0, None, None, None,
+                                       None))
 
-    def _rows(self, t: torch.Tensor, what: str):
-        """(rows, tokens, elements between rows) of [...][experts]."""
-        E = self.experts
-        _check(t.is_cuda and t.dtype in _DTYPES, what + ": a float32, bfloat16 or float16 CUDA tensor")
-        shape = t.shape
-        _check(len(shape) >= 1 and shape[-1] == E, "%s: the last dimension has %d experts" % (what, E))
+    def __reduce__(self):   # copies and pickles by its arguments
+        return Router, (self.experts, self.top_k, self.score, self.normalize, self.scale)
+
+    def _rows(self, t: torch.Tensor):
+        """(configuration, rows, tokens, elements between rows) of logits [...][experts]."""
+        E, shape, cfg = self.experts, t.shape, self._cfg.get(t.dtype)
+        if cfg is None or not t.is_cuda:
+            raise ValueError("logits: a float32, bfloat16 or float16 CUDA tensor")
+        if not shape or shape[-1] != E:
+            raise ValueError("logits: the last dimension has %d experts" % E)
         if len(shape) != 2:
             t = t.reshape(-1, E)
         T, (between, within) = t.shape[0], t.stride()
-        _check(E == 1 or within == 1, what + ": experts of a token are adjacent")
-        _check(T <= 1 or between >= E, what + ": rows do not overlap")
-        return t, T, between if T > 1 else E
+        if within != 1 and E > 1:
+            raise ValueError("logits: experts of a token are adjacent")
+        if T <= 1:
+            between = E
+        elif between < E:
+            raise ValueError("logits: rows do not overlap")
+        return cfg, t, T, between
 
     def forward(self, logits: torch.Tensor, bias: Optional[torch.Tensor] = None,
                 mask: Optional[torch.Tensor] = None, stream=None):
@@ -118,49 +133,54 @@ class Router:
 
         bias [experts] float32 is added to the sigmoid scores for the choice alone; mask [...]
         (bool or uint8) leaves out the tokens where it is 0: ids -1, weights 0."""
-        rows, T, stride = self._rows(logits, "logits")
-        index = rows.get_device()
-        if bias is not None:
-            _check(bias.dtype == torch.float32 and bias.is_contiguous() and
-                   bias.get_device() == index and bias.shape == (self.experts,),
-                   "bias: [experts] float32, contiguous, on the logits' device")
-        if mask is not None:
-            _check(mask.dtype in (torch.bool, torch.uint8) and mask.is_contiguous() and
-                   mask.get_device() == index and mask.shape == logits.shape[:-1],
-                   "mask: bool or uint8, contiguous, one value a token, on the logits' device")
+        cfg, rows, T, between = self._rows(logits)
+        index, lead = rows.get_device(), logits.shape[:-1]
+        if bias is not None and not (bias.dtype is torch.float32 and bias.is_contiguous() and
+                                     bias.get_device() == index and bias.shape == (self.experts,)):
+            raise ValueError("bias: [experts] float32, contiguous, on the logits' device")
+        if mask is not None and not (mask.dtype in (torch.bool, torch.uint8) and
+                                     mask.is_contiguous() and mask.get_device() == index and
+                                     mask.shape == lead):
+            raise ValueError("mask: bool or uint8, contiguous, one value a token, on the logits' "
+                             "device")
         if not _at_home(index, stream):
             with _Elsewhere(index, stream, (logits, bias, mask)):
                 return self.forward(logits, bias, mask)
-        want = logits.shape[:-1] + (self.top_k,)
+        want = (*lead, self.top_k)
         ids = rows.new_empty(want, dtype=torch.int32)
         weights = rows.new_empty(want, dtype=torch.float32)
-        _raise(B.topoep_router_forward(self._cfg[rows.dtype], rows.data_ptr(), stride, T,
-                                       bias.data_ptr() if bias is not None else None,
-                                       mask.data_ptr() if mask is not None else None,
-                                       ids.data_ptr(), weights.data_ptr(), _current_raw(index)))
+        rc = self._forward(cfg, rows.data_ptr(), between, T,
+                           None if bias is None else bias.data_ptr(),
+                           None if mask is None else mask.data_ptr(),
+                           ids.data_ptr(), weights.data_ptr(), _current_raw(index))
+        if rc:
+            raise B.TopoEPError(rc)
         return ids, weights
 
     def backward(self, logits: torch.Tensor, ids: torch.Tensor, weights: torch.Tensor,
                  grad_weights: torch.Tensor, stream=None) -> torch.Tensor:
         """Gradient of the logits (their type and shape) from the gradient of the weights."""
-        rows, T, stride = self._rows(logits, "logits")
-        index, want = rows.get_device(), logits.shape[:-1] + (self.top_k,)
-        _check(ids.dtype == torch.int32 and ids.is_contiguous() and ids.shape == want and
-               ids.get_device() == index, "ids: as forward() returned them")
-        _check(weights.dtype == torch.float32 and weights.is_contiguous() and
-               weights.shape == want and weights.get_device() == index,
-               "weights: as forward() returned them")
-        _check(grad_weights.dtype == torch.float32 and grad_weights.shape == want and
-               grad_weights.get_device() == index, "grad_weights: float32, shaped as the weights")
+        cfg, rows, T, between = self._rows(logits)
+        index, want = rows.get_device(), (*logits.shape[:-1], self.top_k)
+        if not (ids.dtype is torch.int32 and ids.is_contiguous() and ids.shape == want and
+                ids.get_device() == index):
+            raise ValueError("ids: as forward() returned them")
+        if not (weights.dtype is torch.float32 and weights.is_contiguous() and
+                weights.shape == want and weights.get_device() == index):
+            raise ValueError("weights: as forward() returned them")
+        if not (grad_weights.dtype is torch.float32 and grad_weights.shape == want and
+                grad_weights.get_device() == index):
+            raise ValueError("grad_weights: float32, shaped as the weights")
         if not _at_home(index, stream):
             with _Elsewhere(index, stream, (logits, ids, weights, grad_weights)):
                 return self.backward(logits, ids, weights, grad_weights)
         grad_weights = grad_weights.contiguous()
         grad = rows.new_empty(logits.shape)
-        _raise(B.topoep_router_backward(self._cfg[rows.dtype], rows.data_ptr(), stride, T,
-                                        ids.data_ptr(), weights.data_ptr(),
-                                        grad_weights.data_ptr(), grad.data_ptr(), self.experts,
-                                        _current_raw(index)))
+        rc = self._backward(cfg, rows.data_ptr(), between, T, ids.data_ptr(), weights.data_ptr(),
+                            grad_weights.data_ptr(), grad.data_ptr(), self.experts,
+                            _current_raw(index))
+        if rc:
+            raise B.TopoEPError(rc)
         return grad
 
     def __call__(self, logits: torch.Tensor, bias: Optional[torch.Tensor] = None,
@@ -188,6 +208,7 @@ class TokenExperts:
         if self.device.index is None:
             self.device = torch.device("cuda", torch.cuda.current_device())
         self._index = self.device.index
+        self._forward = B.lib().topoep_experts_forward
         self._params = None
         nbytes = B.topoep_experts_workspace_bytes(handle)
         with torch.cuda.device(self.device):
@@ -230,35 +251,42 @@ class TokenExperts:
                 out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
         """y [tokens][hidden] bfloat16 of x [tokens][hidden] bfloat16, instance ids [tokens][top_k]
         int32 (the plan's token_replica rows) and weights [tokens][top_k] float32."""
-        _check(x.dim() == 2 and x.dtype == torch.bfloat16 and x.shape[1] == self.hidden and
-               x.get_device() == self._index, "x: [tokens][hidden] bfloat16 on this device")
+        index, H = self._index, self.hidden
+        if not (x.dim() == 2 and x.dtype is torch.bfloat16 and x.shape[1] == H and
+                x.get_device() == index):
+            raise ValueError("x: [tokens][hidden] bfloat16 on this device")
         T, (between, within) = x.shape[0], x.stride()
-        _check(T <= self.max_tokens, "at most %d tokens" % self.max_tokens)
-        _check(self.hidden == 1 or within == 1, "x: elements of a row are adjacent")
-        _check(T <= 1 or between >= self.hidden or between == 0, "x: rows do not overlap")
+        if T > self.max_tokens:
+            raise ValueError("at most %d tokens" % self.max_tokens)
+        if within != 1 and H > 1:
+            raise ValueError("x: elements of a row are adjacent")
+        if T > 1 and 0 < between < H:
+            raise ValueError("x: rows do not overlap")
         want = (T, self.top_k)
-        _check(ids.dtype == torch.int32 and ids.is_contiguous() and ids.shape == want and
-               ids.get_device() == self._index,
-               "ids: [tokens][top_k] int32, contiguous, on this device")
-        _check(weights.dtype == torch.float32 and weights.is_contiguous() and
-               weights.shape == want and weights.get_device() == self._index,
-               "weights: [tokens][top_k] float32, contiguous, on this device")
-        if out is not None:
-            _check(out.dtype == torch.bfloat16 and out.shape == (T, self.hidden) and
-                   out.get_device() == self._index and (self.hidden == 1 or out.stride(1) == 1) and
-                   (T <= 1 or out.stride(0) >= self.hidden),
-                   "out: [tokens][hidden] bfloat16 on this device, elements of a row adjacent")
-        if not _at_home(self._index, stream):
-            with _Elsewhere(self._index, stream, (x, ids, weights, out)):
+        if not (ids.dtype is torch.int32 and ids.is_contiguous() and ids.shape == want and
+                ids.get_device() == index):
+            raise ValueError("ids: [tokens][top_k] int32, contiguous, on this device")
+        if not (weights.dtype is torch.float32 and weights.is_contiguous() and
+                weights.shape == want and weights.get_device() == index):
+            raise ValueError("weights: [tokens][top_k] float32, contiguous, on this device")
+        if out is not None and not (out.dtype is torch.bfloat16 and out.shape == (T, H) and
+                                    out.get_device() == index and (H == 1 or out.stride(1) == 1) and
+                                    (T <= 1 or out.stride(0) >= H)):
+            raise ValueError("out: [tokens][hidden] bfloat16 on this device, elements of a row "
+                             "adjacent")
+        if not _at_home(index, stream):
+            with _Elsewhere(index, stream, (x, ids, weights, out)):
                 return self.forward(x, ids, weights, out)
-        if T > 1 and between == 0:   # one row for every token
-            x, between = x.contiguous(), self.hidden
+        if T <= 1:
+            between = H
+        elif between == 0:   # one row for every token
+            x, between = x.contiguous(), H
         if out is None:
-            out = x.new_empty((T, self.hidden))
-        _raise(B.topoep_experts_forward(self.handle, x.data_ptr(), between if T > 1 else self.hidden,
-                                        ids.data_ptr(), weights.data_ptr(), T, out.data_ptr(),
-                                        out.stride(0) if T > 1 else self.hidden,
-                                        _current_raw(self._index)))
+            out = x.new_empty((T, H))
+        rc = self._forward(self.handle, x.data_ptr(), between, ids.data_ptr(), weights.data_ptr(), T,
+                           out.data_ptr(), out.stride(0) if T > 1 else H, _current_raw(index))
+        if rc:
+            raise B.TopoEPError(rc)
         return out
 
     __call__ = forward
@@ -334,6 +362,8 @@ class GradientClip:
         rc, handle = B.topoep_clip_create(table)
         _raise(rc)
         self.handle = handle
+        self._norm, self._run = B.lib().topoep_clip_norm, B.lib().topoep_clip_run
+        self._like = torch.empty(0, dtype=torch.float32, device=self.device)
         nbytes = B.topoep_clip_workspace_bytes(handle)
         with torch.cuda.device(self.device):
             self._workspace, ptr = _workspace(nbytes, self.device)
@@ -363,9 +393,11 @@ class GradientClip:
         if not _at_home(index, stream):
             with _Elsewhere(index, stream, [t for both in self._tensors for t in both]):
                 return self._call(max_norm, None)
-        value = torch.empty((), dtype=torch.float32, device=self.device)
+        value = self._like.new_empty(())
         if max_norm is None:
-            _raise(B.topoep_clip_norm(self.handle, self._kind, value, _current_raw(index)))
+            rc = self._norm(self.handle, self._kind, value.data_ptr(), _current_raw(index))
         else:
-            _raise(B.topoep_clip_run(self.handle, self._kind, max_norm, value, _current_raw(index)))
+            rc = self._run(self.handle, self._kind, max_norm, value.data_ptr(), _current_raw(index))
+        if rc:
+            raise B.TopoEPError(rc)
         return value

@@ -109,3 +109,17 @@ def test_clip_refuses_a_gradient_listed_twice():
     assert rc((P, 4 * P, 1, 8, 8), (2 * P, 4 * P, 1, 8, 8)) == -10
     assert rc((P, None, 4, 8, 16), (P + 32, None, 4, 8, 16)) == 0       # two halves of rows
     assert rc((P, None, 4, 8, 16), (P, None, 4, 8, 16)) == -10
+
+
+def test_router_copies_by_its_arguments():
+    import copy
+    import pickle
+    from paper_2609_35481_b200 import Router
+    r = Router(16, 2, score="sigmoid", normalize=False, scale=2.5)
+    for c in (copy.deepcopy(r), pickle.loads(pickle.dumps(r))):
+        assert (c.experts, c.top_k, c.score, c.normalize, c.scale) == (16, 2, "sigmoid", False, 2.5)
+    for bad in (dict(experts=4, top_k=8), dict(experts=4, top_k=2, scale=0.0)):
+        with pytest.raises(B.TopoEPError):
+            Router(**bad)
+    with pytest.raises(ValueError):
+        Router(4, 2, score="relu")

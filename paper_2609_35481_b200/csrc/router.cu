@@ -14,9 +14,10 @@ namespace {
 
 constexpr int kRouterThreads = 128;
 constexpr int kRouterBlocksPerSm = 8, kBackwardBlocksPerSm = 12, kSparseBlocksPerSm = 12;
-// Up to so many tokens an SM a whole warp takes a token, beyond that eight lanes do (more than 64
-// experts): 4096 tokens of 256 experts 4.4 against 4.1 us, with a bias 5.3 against 7.8; one token 3.1
-// against 3.3, with a bias 3.6 against 6.7; 16384 tokens 12.9 against 7.7.
+// A whole warp takes a token while the SMs' 32 warps hold all tokens at once, half a warp while twice
+// as many (129 to 256 experts), and eight lanes beyond (more than 64 experts).  256 experts,
+// with a bias: 4096 tokens 5.3 us, with eight lanes 7.8; 8192 tokens 6.3 with sixteen, 7.8 with eight;
+// 16384 tokens 11.7 with sixteen, 11.1 with eight.  Without one: 4.4, 4.1; 4.7, 4.9; 8.9, 7.8.
 constexpr int kFew = 32;
 constexpr float kSigmoidEps = 1e-20f;
 
@@ -549,9 +550,10 @@ cudaError_t launch_forward(const RouterParams& p, int sms, cudaStream_t stream) 
   const bool few = p.tokens <= kFew * sms;
   if (p.E <= 32) return launch_forward_rows<T, 8, 4>(p, sms, stream);
   if (p.E <= 64) return launch_forward_rows<T, 8, 8>(p, sms, stream);
+  if (p.E <= 128) return few ? launch_forward_rows<T, 32, 8>(p, sms, stream) : launch_forward_rows<T, 8, 16>(p, sms, stream);
   if (few && p.E <= 256) return launch_forward_rows<T, 32, 8>(p, sms, stream);
+  if (p.tokens <= 2 * kFew * sms && p.E <= 256) return launch_forward_rows<T, 16, 16>(p, sms, stream);
   if (few && p.E <= 512) return launch_forward_rows<T, 32, 16>(p, sms, stream);
-  if (p.E <= 128) return launch_forward_rows<T, 8, 16>(p, sms, stream);
   if (p.E <= 256) return launch_forward_rows<T, 8, 32>(p, sms, stream);
   if (p.E <= 512) return launch_forward_rows<T, 16, 32>(p, sms, stream);
   if (p.E <= 1024) return launch_forward_rows<T, 32, 32>(p, sms, stream);

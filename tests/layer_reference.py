@@ -40,6 +40,31 @@ def router_forward(logits, k, score, normalize, scale, bias=None, mask=None):
     return ids, w
 
 
+def router_forward_many(logits, k, score, normalize, scale, bias=None, mask=None):
+    """router_forward for many tokens at once, with a stable sort.  Among so many a 32-bit choice
+    value one unit off would swap two experts now and then, and exp differs by a unit between
+    libraries: it is formed where the logits are."""
+    l32 = logits.float().cpu()
+    choice = l32 if bias is None else \
+        (1.0 / (1.0 + torch.exp(-logits.float())) + bias.float()).cpu()
+    choice = torch.where((l32 == -math.inf) | torch.isnan(choice), -math.inf, choice)
+    value, ids = torch.sort(choice, dim=1, descending=True, stable=True)
+    value, ids = value[:, :k], ids[:, :k]
+    taken = value != -math.inf
+    if mask is not None:
+        taken &= mask.cpu().bool()[:, None]
+    z, picked = l32.double(), l32.double().gather(1, ids)
+    if score == "sigmoid":
+        w = torch.where(taken, torch.special.expit(picked), 0.0)
+        w = w / (w.sum(1, keepdim=True) + 1e-20) if normalize else w
+    else:
+        over = torch.where(taken, picked, -math.inf) if normalize else z
+        top = over.amax(1, keepdim=True).clamp(min=-3.5e38)
+        w = torch.exp(picked - top) / torch.exp(over - top).sum(1, keepdim=True)
+    w = torch.where(taken, scale * w, 0.0)
+    return torch.where(taken, ids, -1).int(), w
+
+
 def router_weight_bound(logits, weights, E):
     """exp and its argument lose a few units and, by the rounding of the argument's product, as
     many more as the logits are apart; the sum of E terms and the divisions the rest."""

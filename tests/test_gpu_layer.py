@@ -58,6 +58,32 @@ def test_router_forward_and_backward(T, E, k, dtype, score, normalize):
     check_router_grad(r, logits, ids, w, 3)
 
 
+@pytest.mark.parametrize("score,normalize,biased", [("softmax", True, False), ("softmax", False, False),
+                                                    ("sigmoid", True, True)])
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("T,E,k", [(5001, 100, 8), (5003, 160, 7), (5002, 256, 8), (9601, 256, 8),
+                                   (9603, 200, 32), (9700, 257, 8), (5001, 512, 8), (5001, 64, 6),
+                                   (5001, 30, 4)])
+def test_router_many_tokens_with_special_rows_among_them(T, E, k, dtype, score, normalize, biased):
+    """The forms for more tokens than warps; rows with many ties, masked experts and nothing left
+    share a warp with ordinary ones."""
+    g = gen(T + E)
+    logits = (2.0 * torch.randn(T, E, generator=g, device="cuda")).to(dtype)
+    logits[::7] = 0.25                                   # all equal
+    logits[3::11, ::2] = -INF
+    logits[5::13] = -INF                                 # nothing left
+    logits[8::17] = torch.randint(0, 3, (E,), generator=g, device="cuda").to(dtype)
+    mask = torch.rand(T, generator=g, device="cuda") < 0.9
+    bias = 0.2 * torch.randn(E, generator=g, device="cuda") if biased else None
+    r = Router(E, k, score=score, normalize=normalize, scale=1.5)
+    for rows in (logits, torch.cat([logits, logits[:, :3]], 1)[:, :E]):   # the second one not vectors
+        ids, w = r.forward(rows, bias=bias, mask=mask)
+        want_ids, want_w = ref.router_forward_many(logits, k, score, normalize, 1.5, bias, mask)
+        assert torch.equal(ids.cpu(), want_ids)
+        bound = ref.router_weight_bound(logits, want_w, E)
+        assert ((w.cpu().double() - want_w).abs() <= bound).all()
+
+
 @pytest.mark.parametrize("T,E,k,dtype", [(300, 256, 8, F32), (65, 64, 6, BF16), (20, 2000, 8, F32),
                                          (77, 40, 40 - 8, F16)])
 def test_router_bias_moves_the_choice_and_not_the_weights(T, E, k, dtype):

@@ -787,8 +787,10 @@ experts_kernel(const __grid_constant__ Maps maps, const __grid_constant__ LayerP
   if (failed_shared) {   // a wait ran out: report it and let the copies in flight land
     if (tid == 0) {
       atomicOr(p.control + C_STATUS, TOPOEP_FLAG_INTERNAL);
-      for (int s = 0; s < stages; ++s)
-        if (!mbar_wait(full + 8 * s, 0)) mbar_wait(full + 8 * s, 1);
+      for (int s = 0; s < stages; ++s) {   // one of the two is the use that may still be under way
+        mbar_wait(full + 8 * s, 0);
+        mbar_wait(full + 8 * s, 1);
+      }
     }
     __syncthreads();
   }

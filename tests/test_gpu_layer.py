@@ -339,6 +339,22 @@ def test_experts_all_rows_on_one_instance_and_every_count():
     check_experts(128, 4, 1, 5, 0, 136, 200, ids=ids, seed=4)
 
 
+@pytest.mark.parametrize("slots,H,F,T", [(18, 256, 1024, 24), (37, 128, 512, 40), (38, 192, 512, 20),
+                                         (60, 128, 640, 33), (75, 72, 520, 128), (148, 64, 256, 40),
+                                         (7, 520, 128, 9)])
+def test_experts_every_way_of_dealing_out_tiles(slots, H, F, T):
+    """On 148 SMs: all tiles whole, exactly one a block, one and a few cut, several rounds and a rest
+    cut or whole, a second product with more tiles than the first."""
+    g = gen(slots)
+    k = -(-slots // T) + 2
+    ids = torch.full((T, k), -1, dtype=torch.int32, device="cuda")
+    ids.view(-1)[torch.randperm(T * k, generator=g, device="cuda")[:slots]] = \
+        torch.arange(slots, dtype=torch.int32, device="cuda")            # every instance once
+    extra = torch.randint(0, slots, (T,), generator=g, device="cuda", dtype=torch.int32)
+    ids[:, -1] = torch.where(ids[:, -1] < 0, extra, ids[:, -1])          # and some again
+    check_experts(T, k, 1, slots, 0, H, F, seed=slots, ids=ids)
+
+
 def test_experts_longer_layers():
     check_experts(2, 2, 1, 3, 1, 4096, 1408, seed=5)
     check_experts(20, 2, 1, 3, 0, 1024, 2048, seed=6)
